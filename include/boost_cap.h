@@ -24,7 +24,7 @@
  *     first call on a tensor or pool may be made inside HIP graph capture.
  *     Two decode calls that use the same tensor or pool must be ordered on one
  *     stream (they share the tensor's split-row scratch).
- *   - Allocator calls (boost_kv_alloc / boost_kv_free) are CPU-only
+ *   - Allocator calls (boost_kv_alloc, boost_kv_free and those beside them) are CPU-only
  *     bookkeeping and are not thread-safe: one scheduler thread per pool.
  */
 #ifndef BOOST_CAP_H
@@ -451,8 +451,43 @@ typedef struct boost_kv_usage {
  * page), ENOMEM, EHIP. */
 int boost_kv_pool_create(boost_ctx *ctx, const boost_kv_cfg *cfg,
                          boost_kv_pool **out);
+
+/* Formats of the cached keys and values (reading beside the paper, whose
+ * pools are 16 bits wide: the same pages carry 3.76 times the tokens).
+ *   BOOST_KV_BF16: the values as they are written.
+ *   BOOST_KV_FP4: microscaled 4-bit floating point, head_dim 128.  The 128
+ *     values of a token and KV head are four groups of 32 consecutive dims; a
+ *     group is stored as E2M1 codes (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their
+ *     negatives) times 2^e, e the smallest with max|x| <= 7 * 2^e within
+ *     [-127, 125]; values are rounded to the nearest code, ties to the even
+ *     one, and beyond 6 to 6.  A group with an infinity or a NaN reads back as
+ *     NaN in all its dims.  68 bytes instead of 256. */
+#define BOOST_KV_BF16 0
+#define BOOST_KV_FP4 1
+
+/* boost_kv_pool_create (which is BOOST_KV_BF16) with a format.  Every call
+ * that takes a pool works on both: tokens are handed over and returned as
+ * bf16, and attention over a 4-bit pool computes with the values that the
+ * codes stand for (q exact, sums and softmax in fp32; probabilities enter the
+ * product with V in parts that keep 24 significant bits up to five query
+ * heads per KV head, 16 above).  In a 4-bit pool blocks_per_page is 1920, and
+ * attention takes any q_heads / kv_heads up to 8.
+ * Errors: as boost_kv_pool_create; EINVAL (format, head_dim). */
+int boost_kv_pool_create_format(boost_ctx *ctx, const boost_kv_cfg *cfg, int format,
+                                boost_kv_pool **out);
+int boost_kv_pool_format(const boost_kv_pool *pool, int *format);
+
 int boost_kv_pool_info(const boost_kv_pool *pool, boost_kv_info *info);
 int boost_kv_pool_destroy(boost_kv_pool *pool);
+
+/* Device addresses of the pages of one layer's K (which = 0) or V (1) tensor,
+ * in order: min(pages, cap) of them to addresses (may be NULL with cap 0), the
+ * count to *n_pages.  For views of a cache (all its HBM pages follow one
+ * another: layer by layer, K then V) and for writing it out; what the pages
+ * hold is the pool's, and must not be touched while calls on it run.
+ * Errors: EINVAL, ENODEV. */
+int boost_kv_pages(const boost_kv_pool *pool, int layer, int which, uint64_t *addresses,
+                   uint64_t cap, uint64_t *n_pages);
 
 /* Host heads (0..H) of one block.  Errors: EINVAL (block out of range). */
 int boost_kv_block_host_heads(const boost_kv_pool *pool, int32_t block,
@@ -489,6 +524,14 @@ int boost_kv_stats(const boost_kv_pool *pool, boost_kv_usage *out);
 int boost_kv_write(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
                    const int32_t *slots, const void *k, const void *v, int n,
                    void *stream);
+
+/* Read n tokens of one layer back as bf16 [n, H, D] (swapping a request out,
+ * or handing a cached prefix to a dense computation): row i of k and v gets
+ * the token in slots[i].  Rows of slots outside the pool are left as they are.
+ * k, v: device, 16-byte aligned.  Asynchronous on `stream`.
+ * Errors: EINVAL, ENODEV, EHIP. */
+int boost_kv_read(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
+                  const int32_t *slots, void *k, void *v, int n, void *stream);
 
 /* GQA decode attention over the pool (§3.3 KV head chunks per workgroup;
  * §4.5 paged layout):  for request b and query head h (KV head g = h / (Hq/H))

@@ -20,6 +20,7 @@ _LIB_PATH = os.environ.get("BOOST_LIB") or os.path.join(HERE, "_lib", "libboostc
 OK, EINVAL, ENOMEM, EAGAIN, ENODEV, EHIP = 0, -22, -12, -11, -19, -5
 KV_LPP, KV_ALL_HBM, KV_ALL_HOST, KV_BUDGET = 0, 1, 2, 3
 KV_LOCAL, KV_SHH = 0, 1
+KV_BF16, KV_FP4 = 0, 1
 TIER_HBM, TIER_HOST = 0, 1
 PLACE_MPP, PLACE_MPP_GLOBAL, PLACE_LINEAR, PLACE_RANDOM = 0, 1, 2, 3
 DTYPE_F32, DTYPE_BF16 = 0, 1
@@ -107,6 +108,10 @@ _SIGS = {
     "boost_staged_view": (_i32, [_vp, _vp, _vp, _u64, C.POINTER(_vp)]),
     "boost_prefetch": (_i32, [_vp, _vp, _vp]),
     "boost_kv_pool_create": (_i32, [_vp, C.POINTER(KVCfg), C.POINTER(_vp)]),
+    "boost_kv_pool_create_format": (_i32, [_vp, C.POINTER(KVCfg), _i32, C.POINTER(_vp)]),
+    "boost_kv_pool_format": (_i32, [_vp, C.POINTER(_i32)]),
+    "boost_kv_pages": (_i32, [_vp, _i32, _i32, _vp, _u64, C.POINTER(_u64)]),
+    "boost_kv_read": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp]),
     "boost_kv_pool_info": (_i32, [_vp, C.POINTER(KVInfo)]),
     "boost_kv_pool_destroy": (_i32, [_vp]),
     "boost_kv_block_host_heads": (_i32, [_vp, C.c_int32, C.POINTER(_u32)]),
@@ -426,6 +431,33 @@ def boost_kv_pool_create(ctx: int, layers: int, kv_heads: int, head_dim: int,
     return h.value
 
 
+def boost_kv_pool_create_format(ctx: int, fmt: int, layers: int, kv_heads: int, head_dim: int,
+                                n_blocks: int, M: int, tier_mode: int = KV_LPP,
+                                q_heads: int = 0, max_batch: int = 0,
+                                max_blocks_per_seq: int = 0, block_tokens: int = 16,
+                                hbm_budget_bytes: int = 0) -> int:
+    cfg = KVCfg(layers, kv_heads, head_dim, block_tokens, n_blocks, M, tier_mode,
+                q_heads or kv_heads, max_batch, max_blocks_per_seq, hbm_budget_bytes)
+    h = _vp()
+    _check(load().boost_kv_pool_create_format(ctx, C.byref(cfg), fmt, C.byref(h)))
+    return h.value
+
+
+def boost_kv_pool_format(pool: int) -> int:
+    f = _i32()
+    _check(load().boost_kv_pool_format(pool, C.byref(f)))
+    return f.value
+
+
+def boost_kv_pages(pool: int, layer: int, which: int) -> np.ndarray:
+    """Device addresses of the pages of a layer's K (0) or V (1) tensor."""
+    n = _u64()
+    _check(load().boost_kv_pages(pool, layer, which, None, 0, C.byref(n)))
+    out = np.zeros(n.value, dtype=np.uint64)
+    _check(load().boost_kv_pages(pool, layer, which, _ptr(out), out.size, C.byref(n)))
+    return out
+
+
 def boost_kv_pool_info(pool: int) -> dict:
     i = KVInfo()
     _check(load().boost_kv_pool_info(pool, C.byref(i)))
@@ -471,6 +503,11 @@ def boost_kv_stats(pool: int) -> dict:
 def boost_kv_write(ctx: int, pool: int, layer: int, slots, k, v, n: int, stream=None):
     _check(load().boost_kv_write(ctx, pool, layer, _ptr(slots), _ptr(k), _ptr(v), n,
                                  _stream(stream)))
+
+
+def boost_kv_read(ctx: int, pool: int, layer: int, slots, k, v, n: int, stream=None):
+    _check(load().boost_kv_read(ctx, pool, layer, _ptr(slots), _ptr(k), _ptr(v), n,
+                                _stream(stream)))
 
 
 def boost_paged_attn_decode(ctx: int, pool: int, layer: int, q, B: int, Hq: int,

@@ -21,7 +21,7 @@
 #include <cmath>
 #include <mutex>
 
-#include "runtime.h"
+#include "attn_items.h"
 
 namespace bst {
 int kv_parts_for(const boost_kv_pool* p, int max_blocks);
@@ -29,63 +29,15 @@ int kv_parts_for(const boost_kv_pool* p, int max_blocks);
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kD = 128;          // head dimension of this kernel
-constexpr int kT = 16;           // tokens per block
+using namespace bst::attn;
+
 constexpr int kLanesTok = kD / 8;  // lanes per token row (16)
 #ifndef BOOST_ATTN_UNROLL
 #define BOOST_ATTN_UNROLL 4
 #endif
-// Work items a launch aims for (partition size follows; config 3: 2048
-// items of 64 blocks ran 120 us against 122 us with 4096 of 32)
-#ifndef BOOST_ATTN_ITEMS
-#define BOOST_ATTN_ITEMS 2048
-#endif
 #ifndef BOOST_ATTN_UNROLL8
 #define BOOST_ATTN_UNROLL8 BOOST_ATTN_UNROLL
 #endif
-constexpr int kMaxPartBlocks = 256;         // blocks per partition, at most
-static_assert(kMaxPartBlocks <= kThreads, "one thread per partition size");
-// A work item of fewer than 16 blocks spends as long on its start (q loads)
-// and end (slot merge, partial stores) as on its K/V (batch 8 at 2048 tokens:
-// 1.2 TB/s with 4-block items, 2.2 TB/s with 16).
-#ifndef BOOST_ATTN_PART_MIN
-#define BOOST_ATTN_PART_MIN 16
-#endif
-#ifndef BOOST_ATTN_PART_MAX
-#define BOOST_ATTN_PART_MAX 256
-#endif
-constexpr int kPartMin = BOOST_ATTN_PART_MIN, kPartMax = BOOST_ATTN_PART_MAX;
-// ... but while such items are fewer than the compute units they are halved,
-// down to four blocks: a longer chain of loads on some units is then worse
-// than the starts and ends of more items (32 / 8 heads, one request of 500 /
-// 2048 tokens: 16.6 / 17.1 -> 10.0 / 11.6 us, four of 200..1000: 16.8 -> 11.4;
-// with enough items it loses, one of 8192: 19.2 -> 20.7).  The items are
-// counted from the width of the block table, since the host does not know the
-// context lengths: short contexts in a wide table keep kPartMin.
-constexpr int kPartFew = 4;
-
-struct AttnParams {
-  // Linear placement makes the tier of a pool page a fixed function of its
-  // offset: pages [0, first_host) of a tensor are consecutive in the HBM slab
-  // and pages [first_host, pages) consecutive in the host slab.
-  const char* k_hbm;   // this layer's K tensor: first HBM page
-  const char* k_host;  // ... first host page
-  const char* v_hbm;
-  const char* v_host;
-  uint64_t host_from;  // byte offset where the tensor's host tail begins
-  const uint16_t* q;      // [B, Hq, D]
-  const int32_t* tables;  // [B, max_blocks]
-  const int32_t* lens;    // [B]
-  int B, H, Hq, nb, max_blocks;
-  int part_blocks, n_parts;  // partition size in blocks, partitions per request
-  int max_parts;             // stride of the partial buffers
-  float scale;
-  float* part_acc;  // [B * Hq * max_parts][D] unnormalised sums of p * v
-  float* part_ml;   // [B * Hq * max_parts][2] running max, sum of p
-  void* out;
-  int out_bf16;
-};
 
 __device__ __forceinline__ float lo_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t v) {
@@ -97,13 +49,6 @@ __device__ __forceinline__ void unpack8(const uint4& u, float* f) {
   f[2] = lo_bf16(u.y); f[3] = hi_bf16(u.y);
   f[4] = lo_bf16(u.z); f[5] = hi_bf16(u.z);
   f[6] = lo_bf16(u.w); f[7] = hi_bf16(u.w);
-}
-
-__device__ __forceinline__ uint16_t to_bf16(float f) {
-  uint32_t u = __float_as_uint(f);
-  if ((u & 0x7f800000u) == 0x7f800000u && (u & 0x007fffffu)) return 0x7fc0;
-  u += 0x7fffu + ((u >> 16) & 1u);
-  return static_cast<uint16_t>(u >> 16);
 }
 
 __device__ __forceinline__ uint4 load_block(const char* base, bool ok, uint32_t off) {
@@ -387,212 +332,6 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
   }
 }
 
-// Blocks of request b in this call (0 for an empty context).
-__device__ __forceinline__ int blocks_of(const AttnParams& P, int b) {
-  const int L = P.lens[b];
-  return L <= 0 ? 0 : min((L + kT - 1) / kT, P.max_blocks);
-}
-
-// Sum of v over the workgroup; every thread gets it (red: 4 ints of LDS).
-__device__ __forceinline__ int wg_sum(int v, int* red) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) v += __shfl_xor(v, m, 64);
-  __syncthreads();  // red is free again
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return red[0] + red[1] + red[2] + red[3];
-}
-
-// Exclusive prefix sum of v over the workgroup in thread order; total gets
-// the sum of every thread's v.
-__device__ __forceinline__ int wg_scan(int v, int* red, int& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int x = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) red[wave] = x;
-  __syncthreads();
-  int before = 0;
-  for (int w = 0; w < wave; ++w) before += red[w];
-  total = red[0] + red[1] + red[2] + red[3];
-  return before + x - v;
-}
-
-// Request whose count interval holds `target` in the running sum of
-// count(n_b) over b = 0, 1, ... (count > 0 there); pick[0] gets b, pick[1]
-// target minus the sum before b, pick[4] b's context length.  n0, L0: this
-// thread's n_b and length for b = threadIdx.x (read once by the caller);
-// later chunks read the lengths again.
-template <typename Count>
-__device__ __forceinline__ void find_request(const AttnParams& P, int target, int n0, int L0,
-                                             Count count, int* red, int* pick) {
-  int carry = 0;
-  for (int base = 0; base < P.B; base += kThreads) {  // uniform
-    const int b = base + static_cast<int>(threadIdx.x);
-    const int c = b < P.B ? count(base == 0 ? n0 : blocks_of(P, b)) : 0;
-    int total;
-    const int ex = carry + wg_scan(c, red, total);
-    if (c > 0 && ex <= target && target < ex + c) {
-      pick[0] = b;
-      pick[1] = target - ex;
-      pick[4] = base == 0 ? L0 : P.lens[b];
-    }
-    carry += total;
-    if (carry > target) break;  // uniform
-  }
-  __syncthreads();
-}
-
-// The item of item_of (below) for at most 64 requests: one request per lane,
-// every wavefront by itself, with ballots instead of barriers (0.9 us less
-// before an item's first loads).
-__device__ __forceinline__ bool item_of_wave(const AttnParams& P, int idx, int& b, int& g,
-                                             int& part, int& L) {
-  const int lane = threadIdx.x & 63, PB = P.part_blocks, H = P.H;
-  const int L0 = lane < P.B ? P.lens[lane] : 0;
-  const int n = L0 <= 0 ? 0 : min((L0 + kT - 1) / kT, P.max_blocks);
-  const int full = n / PB, rem = n % PB;
-  // inclusive prefix sums of both counts over the requests
-  int xf = full, xr = rem > 0;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int yf = __shfl_up(xf, d, 64), yr = __shfl_up(xr, d, 64);
-    if (lane >= d) {
-      xf += yf;
-      xr += yr;
-    }
-  }
-  const int F = __builtin_amdgcn_readlane(xf, 63), R = __builtin_amdgcn_readlane(xr, 63);
-  auto pick = [&](unsigned long long who) {
-    b = __builtin_amdgcn_readfirstlane(static_cast<int>(__ffsll(who)) - 1);
-    L = __builtin_amdgcn_readlane(L0, b);
-  };
-  if (idx < F + R) {  // every partition of head H-1
-    const int end = xf + xr, beg = end - full - (rem > 0);
-    const unsigned long long who = __ballot(beg <= idx && idx < end);
-    if (!who) return false;
-    pick(who);
-    part = idx - __builtin_amdgcn_readlane(beg, b);
-    g = H - 1;
-    return true;
-  }
-  int j = idx - (F + R);
-  if (j < (H - 1) * F) {  // full partitions of the others
-    const int t = j / (H - 1);
-    const unsigned long long who = __ballot(xf - full <= t && t < xf);
-    if (!who) return false;
-    pick(who);
-    part = t - __builtin_amdgcn_readlane(xf - full, b);
-    g = H - 2 - j % (H - 1);
-    return true;
-  }
-  j -= (H - 1) * F;
-  if (j >= (H - 1) * R) return false;
-  // partial partitions by size: the rank-th largest rem (below 256), bit by
-  // bit, then the requests of that size in order
-  int rank = j / (H - 1);
-  unsigned long long who = __ballot(rem > 0);
-#pragma unroll
-  for (int bit = 7; bit >= 0; --bit) {
-    const unsigned long long ones = who & __ballot(rem >> bit & 1);
-    const int c = __popcll(ones);
-    if (rank < c) {
-      who = ones;
-    } else {
-      rank -= c;
-      who &= ~ones;
-    }
-  }
-  const int before = __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(who >> 32),
-                                               __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(who), 0));
-  const unsigned long long one = __ballot((who >> lane & 1) && before == rank);
-  if (!one) return false;
-  pick(one);
-  part = __builtin_amdgcn_readlane(full, b);
-  g = H - 2 - j % (H - 1);
-  return true;
-}
-
-// Work item of workgroup idx, from the context lengths alone (so the same on
-// every pool: the order decides which items run together, never what an item
-// computes).  With n_b blocks, request b has full_b = n_b / part_blocks full
-// partitions and one partial one if rem_b = n_b % part_blocks > 0.  Order:
-//   1. every partition of head H-1 (where host data can lie), request by
-//      request: its slow reads start first;
-//   2. full partitions of heads H-2..0, request by request, head fastest;
-//   3. partial partitions of heads H-2..0, the largest first (rem_b
-//      descending, then b ascending), head fastest;
-//   4. workgroups past the last item return at once.
-// Empty partitions get no workgroup and the short ones run last, so the last
-// grid wave is short (config 3, reads alone: 104 -> 96 us).
-// L gets the request's context length (so the caller does not read it again).
-__device__ bool item_of(const AttnParams& P, int idx, int& b, int& g, int& part, int& L,
-                        int* red, int* hist, int* pick) {
-  const int tid = threadIdx.x, PB = P.part_blocks, H = P.H;
-  if (tid < 5) pick[tid] = -1;  // written by the sums' barriers below
-  const int L0 = tid < P.B ? P.lens[tid] : 0;  // request tid, read once
-  const int n0 = L0 <= 0 ? 0 : min((L0 + kT - 1) / kT, P.max_blocks);
-  int f = 0, r = 0;
-  for (int bb = tid; bb < P.B; bb += kThreads) {
-    const int n = bb == tid ? n0 : blocks_of(P, bb);
-    f += n / PB;
-    r += n % PB > 0;
-  }
-  const int F = wg_sum(f, red), R = wg_sum(r, red);
-  const int S0 = F + R;
-  if (idx < S0) {
-    find_request(P, idx, n0, L0, [&](int n) { return n / PB + (n % PB > 0); }, red, pick);
-    b = pick[0];
-    part = pick[1];
-    L = pick[4];
-    g = H - 1;
-    return b >= 0 && b < P.B && part >= 0;
-  }
-  int j = idx - S0;
-  if (j < (H - 1) * F) {
-    find_request(P, j / (H - 1), n0, L0, [&](int n) { return n / PB; }, red, pick);
-    b = pick[0];
-    part = pick[1];
-    L = pick[4];
-    g = H - 2 - j % (H - 1);
-    return b >= 0 && b < P.B && part >= 0;
-  }
-  j -= (H - 1) * F;
-  if (j >= (H - 1) * R) return false;
-  // partial partitions by size: a counting sort over rem in [1, PB)
-  const int rank = j / (H - 1);
-  for (int v = tid; v < PB; v += kThreads) hist[v] = 0;
-  __syncthreads();
-  for (int bb = tid; bb < P.B; bb += kThreads) {
-    const int rem = (bb == tid ? n0 : blocks_of(P, bb)) % PB;
-    if (rem > 0) atomicAdd(&hist[rem], 1);
-  }
-  __syncthreads();
-  {
-    const int v = PB - 1 - tid;  // thread order = rem descending (PB <= kThreads)
-    const int c = v >= 1 ? hist[v] : 0;
-    int total;
-    const int ex = wg_scan(c, red, total);
-    if (c > 0 && ex <= rank && rank < ex + c) {
-      pick[2] = v;
-      pick[3] = rank - ex;
-    }
-    __syncthreads();
-  }
-  const int vsel = pick[2];
-  find_request(P, pick[3], n0, L0, [&](int n) { return n % PB == vsel ? 1 : 0; }, red, pick);
-  b = pick[0];
-  if (b < 0 || b >= P.B) return false;
-  L = pick[4];
-  part = (L <= 0 ? 0 : min((L + kT - 1) / kT, P.max_blocks)) / PB;
-  g = H - 2 - j % (H - 1);
-  return true;
-}
-
 // Waves per SIMD the register allocator targets: three for G <= 4 (168
 // registers; against the two it picks by itself this took config 3 from 136 to
 // 126 us; four spill and run at 306 us), two for G = 8 (225 registers; the
@@ -602,7 +341,9 @@ __device__ bool item_of(const AttnParams& P, int idx, int& b, int& g, int& part,
 #ifndef BOOST_ATTN_WAVES
 #define BOOST_ATTN_WAVES 3
 #endif
-template <int G, bool WAVE>
+// SEL: the blocks of the KV head's list in place of the whole context (the
+// list's partial block may stand anywhere, so tokens are counted per block).
+template <int G, bool WAVE, bool SEL>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
     G == 8 ? 2 : BOOST_ATTN_WAVES))) void attn_partition(AttnParams P) {
   constexpr int kUnroll = G == 8 ? BOOST_ATTN_UNROLL8 : BOOST_ATTN_UNROLL;  // blocks in flight
@@ -615,6 +356,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   // would put a round trip before every group of K/V loads); before that the
   // item search's counting sort
   __shared__ int32_t row[kMaxPartBlocks];
+  __shared__ int32_t s_tok[SEL ? kMaxPartBlocks : 1];  // tokens that count of each block
   __shared__ int s_red[4], s_pick[5];
   int part, b, g, L;
   if constexpr (WAVE) {
@@ -622,12 +364,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   } else {
     if (!item_of(P, blockIdx.x, b, g, part, L, s_red, row, s_pick)) return;  // uniform
   }
-  const int n_blk = L <= 0 ? 0 : min((L + kT - 1) / kT, P.max_blocks);
+  const int n_blk = L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks);
   const int blk_beg = part * P.part_blocks;
   if (blk_beg >= n_blk) return;  // uniform: empty partition (not produced by item_of)
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
   // leading blocks whose 16 tokens are all inside the context
-  const int nfull = max(0, min(nbp, L / kT - blk_beg));
+  const int nfull = SEL ? nbp : max(0, min(nbp, L / kT - blk_beg));
   const uint64_t head_off = static_cast<uint64_t>(g) * P.nb * (kT * kD * 2);
   // q stays in bf16 pairs for the dot2 instruction
   // (G = 8: in LDS, since the accumulators and a group's K and V leave no
@@ -661,8 +403,12 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   };
   // the partition's width of the table row (entries past the context are
   // read but not used)
-  if (tid < min(P.part_blocks, P.max_blocks - blk_beg))
+  if constexpr (SEL) {
+    if (tid < nbp)
+      row[tid] = selected(P, b, g, blk_beg + tid, L, s_tok[tid]);
+  } else if (tid < min(P.part_blocks, P.max_blocks - blk_beg)) {
     row[tid] = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk_beg + tid];
+  }
   __syncthreads();
 
   const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
@@ -720,17 +466,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       valid[u] = fetch_k(u, kb[u]);
+      if constexpr (SEL) valid[u] = valid[u] && ts < s_tok[u];
       fetch_v(u, vb[u]);
     }
     for (; i + kUnroll <= nfull; i += kUnroll) {
       const bool more = i + 2 * kUnroll <= nfull;  // uniform
       bool all_ok = true;  // uniform: block ids are the same for every lane
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) all_ok = all_ok && valid[u];
+      for (int u = 0; u < kUnroll; ++u)
+        all_ok = all_ok && (SEL ? row[i + u] >= 0 && row[i + u] < P.nb && s_tok[i + u] == kT
+                                : valid[u]);
       auto next_k = [&] {
         if (more)
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) vnext[u] = fetch_k(i + kUnroll + u, kb[u]);
+          for (int u = 0; u < kUnroll; ++u) {
+            vnext[u] = fetch_k(i + kUnroll + u, kb[u]);
+            if constexpr (SEL) vnext[u] = vnext[u] && ts < s_tok[i + kUnroll + u];
+          }
       };
       if constexpr (kHD) {
         if (all_ok)
@@ -761,7 +513,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
       const bool ok = i + u < nbp && fetch_k(i + u, kb[u]);
       if (i + u < nbp) fetch_v(i + u, vb[u]);
       if (i + u >= nbp) kb[u] = vb[u] = make_uint4(0, 0, 0, 0);
-      valid[u] = ok && (blk_beg + i + u) * kT + ts < L;
+      if constexpr (SEL)
+        valid[u] = ok && ts < s_tok[min(i + u, nbp - 1)];
+      else
+        valid[u] = ok && (blk_beg + i + u) * kT + ts < L;
     }
     if constexpr (kHD)
       consume_hd<G, kUnroll, true>(query, kb, vb, valid, sc2, b0, b1, mh, lh, acc, none);
@@ -833,7 +588,7 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   const int b = bh / P.Hq;
   const int lane = threadIdx.x;
   const int L = P.lens[b];
-  const int n_blk = min((L + kT - 1) / kT, P.max_blocks);
+  const int n_blk = min((L + kT - 1) / kT, P.item_blocks);
   const int np = L <= 0 ? 0 : (n_blk + P.part_blocks - 1) / P.part_blocks;
   const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
   // the largest partition maximum: one partition per lane, then across the
@@ -884,8 +639,8 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   }
 }
 
-template <int G>
-int launch(AttnParams& P, hipStream_t s) {
+template <int G, bool SEL>
+int launch_partitions(AttnParams& P, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
   if (grid > 0x7fffffff) return bst::fail(BOOST_EINVAL, "grid too large");
   // up to 64 requests the search by wavefronts, in a kernel of its own (64
@@ -893,12 +648,21 @@ int launch(AttnParams& P, hipStream_t s) {
   // by barriers, 111.0 with both in one kernel, whose registers spill; one of
   // 8192: 18.5 and 19.4)
   if (P.B <= 64)
-    hipLaunchKernelGGL((attn_partition<G, true>), dim3(static_cast<unsigned>(grid)),
+    hipLaunchKernelGGL((attn_partition<G, true, SEL>), dim3(static_cast<unsigned>(grid)),
                        dim3(kThreads), 0, s, P);
   else
-    hipLaunchKernelGGL((attn_partition<G, false>), dim3(static_cast<unsigned>(grid)),
+    hipLaunchKernelGGL((attn_partition<G, false, SEL>), dim3(static_cast<unsigned>(grid)),
                        dim3(kThreads), 0, s, P);
   BOOST_HIP(hipGetLastError());
+  return BOOST_OK;
+}
+
+template <int G>
+int launch(AttnParams& P, hipStream_t s) {
+  return P.sel ? launch_partitions<G, true>(P, s) : launch_partitions<G, false>(P, s);
+}
+
+int launch_merge(AttnParams& P, hipStream_t s) {
   hipLaunchKernelGGL(attn_merge, dim3(static_cast<unsigned>(P.B * P.Hq)), dim3(64), 0, s, P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
@@ -918,13 +682,13 @@ constexpr int kMaxDevices = 64;
 std::mutex g_scratch_mu;
 float* g_scratch_ptr[kMaxDevices] = {};  // per device: address of `scratch`
 
-// Everything both entry points check and compute, then the two launches;
+// Everything the entry points check and compute, then the two launches;
 // part_acc / part_ml / max_parts name the partial buffers (max_parts = 0:
 // the call's own partition count, with at most cap_rows rows).
 int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, int B, int Hq,
            const int32_t* block_tables, int max_blocks, const int32_t* ctx_lens, float scale,
            void* out, int out_dtype, void* stream, float* part_acc, float* part_ml,
-           int max_parts, int64_t cap_rows) {
+           int max_parts, int64_t cap_rows, const int32_t* sel = nullptr, int top_k = 0) {
   using bst::fail;
   if (!ctx || !pool || !q || !block_tables || !ctx_lens || !out)
     return fail(BOOST_EINVAL, "null argument");
@@ -961,6 +725,9 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   P.Hq = Hq;
   P.nb = static_cast<int>(pool->geom.nb);
   P.max_blocks = max_blocks;
+  P.sel = sel;
+  P.top_k = top_k;
+  P.item_blocks = max_blocks = sel ? std::min(max_blocks, top_k) : max_blocks;
   // enough work items to fill the GPU several times over (so the last grid
   // wave is short), each long enough to amortise its start and its merge
   // (PART_MIN blocks) and short enough to balance (PART_MAX blocks)
@@ -986,13 +753,20 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   P.out = out;
   P.out_bf16 = out_dtype == BOOST_DTYPE_BF16;
   auto s = static_cast<hipStream_t>(stream);
-  switch (G) {
-    case 1: return launch<1>(P, s);
-    case 2: return launch<2>(P, s);
-    case 4: return launch<4>(P, s);
-    case 8: return launch<8>(P, s);
-    default: return fail(BOOST_EINVAL, "Hq/H=%d not in {1, 2, 4, 8}", G);
+  int rc;
+  if (pool->format == BOOST_KV_FP4) {
+    if (G > 8) return fail(BOOST_EINVAL, "Hq/H=%d above 8", G);
+    rc = launch_fp4(P, s);
+  } else {
+    switch (G) {
+      case 1: rc = launch<1>(P, s); break;
+      case 2: rc = launch<2>(P, s); break;
+      case 4: rc = launch<4>(P, s); break;
+      case 8: rc = launch<8>(P, s); break;
+      default: return fail(BOOST_EINVAL, "Hq/H=%d not in {1, 2, 4, 8}", G);
+    }
   }
+  return rc ? rc : launch_merge(P, s);
 }
 
 }  // namespace
@@ -1047,6 +821,19 @@ int boost_paged_attn_decode_noalloc(boost_ctx* ctx, const boost_kv_pool* pool, i
   if (!base) return fail(BOOST_EHIP, "static scratch of device %d not set up", ctx->device);
   return decode(ctx, pool, layer, q, B, Hq, block_tables, max_blocks, ctx_lens, scale, out,
                 out_dtype, stream, base, base + kStaticRows * kD, 0, kStaticRows);
+}
+
+int boost_sparse_attn_decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q,
+                             int B, int Hq, const int32_t* block_tables, int max_blocks,
+                             const int32_t* ctx_lens, const int32_t* sel, int top_k, float scale,
+                             void* out, int out_dtype, void* stream) {
+  if (!pool || !sel) return fail(BOOST_EINVAL, "null argument");
+  if (top_k < 1) return fail(BOOST_EINVAL, "top_k=%d", top_k);
+  const int64_t rows = static_cast<int64_t>(pool->cfg.max_batch) * pool->cfg.q_heads *
+                       std::max(1, pool->max_parts);
+  return decode(ctx, pool, layer, q, B, Hq, block_tables, max_blocks, ctx_lens, scale, out,
+                out_dtype, stream, pool->d_part_acc, pool->d_part_ml,
+                std::max(1, pool->max_parts), rows, sel, top_k);
 }
 
 }  // extern "C"

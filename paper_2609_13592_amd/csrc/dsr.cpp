@@ -8,7 +8,8 @@
 namespace bst {
 
 int kv_geometry(uint32_t n_blocks, uint32_t H, uint32_t D, uint32_t T, uint32_t M,
-                int mode, uint32_t layers, uint64_t hbm_budget_bytes, KvGeom& g) {
+                int mode, uint32_t layers, uint64_t hbm_budget_bytes,
+                uint32_t blocks_per_page, KvGeom& g) {
   if (n_blocks == 0 || H == 0 || D == 0 || T == 0)
     return fail(BOOST_EINVAL, "empty KV geometry");
   if (mode != BOOST_KV_LPP && mode != BOOST_KV_ALL_HBM && mode != BOOST_KV_ALL_HOST &&
@@ -17,13 +18,13 @@ int kv_geometry(uint32_t n_blocks, uint32_t H, uint32_t D, uint32_t T, uint32_t 
   if (mode == BOOST_KV_BUDGET && layers == 0) return fail(BOOST_EINVAL, "0 layers");
   if (mode == BOOST_KV_LPP && M < 2) return fail(BOOST_EINVAL, "M=%u < 2", M);
   const uint64_t hbb = static_cast<uint64_t>(T) * D * 2;  // one head of one block
-  if (kPage % hbb) return fail(BOOST_EINVAL, "head-block of %llu B does not divide a page",
+  if (!blocks_per_page && kPage % hbb) return fail(BOOST_EINVAL, "head-block of %llu B does not divide a page",
                                (unsigned long long)hbb);
   g = KvGeom{};
   g.H = H;
   g.D = D;
   g.T = T;
-  g.blocks_per_page = static_cast<uint32_t>(kPage / hbb);
+  g.blocks_per_page = blocks_per_page ? blocks_per_page : static_cast<uint32_t>(kPage / hbb);
   const uint64_t nb = (static_cast<uint64_t>(n_blocks) + g.blocks_per_page - 1) /
                       g.blocks_per_page * g.blocks_per_page;
   if (nb > 0x7fffffffull) return fail(BOOST_EINVAL, "pool too large");

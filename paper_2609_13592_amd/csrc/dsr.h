@@ -12,7 +12,7 @@ namespace bst {
 
 struct KvGeom {
   uint32_t H = 0, D = 0, T = 0;
-  uint32_t blocks_per_page = 0;  // head-blocks of T*D bf16 per page
+  uint32_t blocks_per_page = 0;  // head-blocks per page
   uint32_t nb = 0;               // pool blocks, a multiple of blocks_per_page
   uint64_t pages = 0;            // pages of one K (or V) tensor: H * nb / bpp
   uint64_t host_pages = 0;       // tail pages on host
@@ -24,9 +24,11 @@ struct KvGeom {
 // Geometry of §4.2 / §4.5: every head's region is whole pages; the last
 // `host_pages` pages of a tensor are on host (1/M of them for LPP; all pages
 // past a per-tensor share of hbm_budget_bytes over `layers` layers of K and V
-// for BOOST_KV_BUDGET).
+// for BOOST_KV_BUDGET).  blocks_per_page: head-blocks of a page in the pool's
+// format (0: those of T * D bf16 values, which must divide the page).
 int kv_geometry(uint32_t n_blocks, uint32_t H, uint32_t D, uint32_t T, uint32_t M,
-                int mode, uint32_t layers, uint64_t hbm_budget_bytes, KvGeom& g);
+                int mode, uint32_t layers, uint64_t hbm_budget_bytes,
+                uint32_t blocks_per_page, KvGeom& g);
 
 // §4.3 wave-aware block fulfillment over two free lists.
 class Dsr {

@@ -6,6 +6,7 @@
 // of attention are bf16 (round to nearest even).
 #include <cmath>
 
+#include "kvfmt.h"
 #include "runtime.h"
 
 namespace {
@@ -281,7 +282,49 @@ struct PoolSlot {
 // copies there), skipped like the append skips a position or block outside
 // the table or the pool.  qkv may come as split-K slices (see slice_value).
 constexpr int kRopeWaves = 4;
-template <bool POOL>
+
+// One head's 128 values in 4 bits, lane i holding dims i (a) and i + 64 (b),
+// already rounded to bf16: the bits kv_write4_kernel stores (layout and
+// scales: kvfmt.h).  The lanes of a half wavefront hold one group each of
+// the lower and the upper dims.
+__device__ __forceinline__ void store_row4(char* page, uint32_t idx, int tok, bool is_v, int i,
+                                           uint16_t a, uint16_t b) {
+  using namespace bst;
+  uint32_t am = a & 0x7fffu, bm = b & 0x7fffu;
+#pragma unroll
+  for (int m = 16; m >= 1; m >>= 1) {
+    am = max(am, static_cast<uint32_t>(__shfl_xor(static_cast<int>(am), m, 64)));
+    bm = max(bm, static_cast<uint32_t>(__shfl_xor(static_cast<int>(bm), m, 64)));
+  }
+  const uint32_t sa = fp4_scale_byte(am << 16), sb = fp4_scale_byte(bm << 16);
+  const float fa = __uint_as_float(static_cast<uint32_t>(a) << 16);
+  const float fb = __uint_as_float(static_cast<uint32_t>(b) << 16);
+  // the other value of this lane's byte: the odd dim of a pair (K), dim + 16 (V)
+  const int far = is_v ? 16 : 1;
+  const float oa = __shfl_xor(fa, far, 64), ob = __shfl_xor(fb, far, 64);
+  const uint32_t ca = fp4_pack<0>(0u, fa, oa, fp4_scale(sa));
+  const uint32_t cb = fp4_pack<0>(0u, fb, ob, fp4_scale(sb));
+  char* const code = page + idx * kFp4Code;
+  const int g = i >> 5;  // groups g and g + 2
+  if (!(i & far)) {
+    if (is_v) {
+      char* const dw = code + (tok / 4) * 256 + (i & 15) * 16 + (tok % 4) * 4;
+      dw[g] = static_cast<char>(ca);
+      dw[g + 2] = static_cast<char>(cb);
+    } else {
+      code[tok * 64 + i / 2] = static_cast<char>(ca);
+      code[tok * 64 + 32 + i / 2] = static_cast<char>(cb);
+    }
+  }
+  if (!(i & 31)) {
+    char* const sc = page + kFp4ScaleAt + idx * kFp4Scale + tok * 4;
+    sc[g] = static_cast<char>(sa);
+    sc[g + 2] = static_cast<char>(sb);
+  }
+}
+
+// FP4: the pool is held in 4 bits (POOL, D = 128: one rotation pair a lane).
+template <bool POOL, bool FP4 = false>
 __global__ __launch_bounds__(64 * kRopeWaves) void rope_qkv_kernel(
     Slices qkv, const int32_t* __restrict__ pos, int Hq, int H, int D, double log2_theta,
     uint16_t* __restrict__ q, uint16_t* __restrict__ k, uint16_t* __restrict__ v, PoolSlot ps) {
@@ -292,7 +335,10 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_qkv_kernel(
   const int lane = threadIdx.x & 63;
   const int half = D / 2;
   const int64_t col0 = static_cast<int64_t>(h) * D;  // this head's first column
-  uint16_t* dst;
+  uint16_t* dst = nullptr;
+  char* page4 = nullptr;  // FP4: the page, index and token of a key or value row
+  uint32_t idx4 = 0;
+  int tok4 = 0;
   if (h < Hq) {
     dst = q + (static_cast<int64_t>(b) * Hq + h) * D;
   } else if constexpr (POOL) {
@@ -301,11 +347,18 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_qkv_kernel(
     const int32_t blk = ps.tables[static_cast<int64_t>(b) * ps.max_blocks + p / ps.T];
     if (blk < 0 || blk >= ps.nb) return;
     const int g = h < Hq + H ? h - Hq : h - Hq - H;
+    if constexpr (FP4) {
+      const bst::Fp4At at = bst::fp4_at(g, blk, ps.nb);
+      page4 = const_cast<char*>((h < Hq + H ? ps.pt_k : ps.pt_v)[at.page]);
+      idx4 = at.idx;
+      tok4 = p % ps.T;
+    }
     // a head row (D * 2 bytes, dividing the page) never crosses a page
     const uint64_t byte = ((static_cast<uint64_t>(g) * ps.nb + blk) * ps.T + p % ps.T) * D * 2;
     const char* const* pt = h < Hq + H ? ps.pt_k : ps.pt_v;
-    dst = reinterpret_cast<uint16_t*>(const_cast<char*>(pt[byte >> 21]) +
-                                      (byte & (bst::kPage - 1)));
+    if constexpr (!FP4)
+      dst = reinterpret_cast<uint16_t*>(const_cast<char*>(pt[byte >> 21]) +
+                                        (byte & (bst::kPage - 1)));
   } else if (h < Hq + H) {
     dst = k + (static_cast<int64_t>(b) * H + (h - Hq)) * D;
   } else {
@@ -314,16 +367,28 @@ __global__ __launch_bounds__(64 * kRopeWaves) void rope_qkv_kernel(
   for (int i = lane; i < half; i += 64) {
     const float a = slice_value(qkv, b, col0 + i), c = slice_value(qkv, b, col0 + i + half);
     if (h >= Hq + H) {
-      dst[i] = to_bf16(a);
-      dst[i + half] = to_bf16(c);
+      if constexpr (FP4) {
+        store_row4(page4, idx4, tok4, true, i, to_bf16(a), to_bf16(c));
+      } else {
+        dst[i] = to_bf16(a);
+        dst[i + half] = to_bf16(c);
+      }
       continue;
     }
     const double inv = exp2(-(2.0 * i / D) * log2_theta);
     const double ang = static_cast<double>(pos[b]) * inv;
     double sn, cs;
     sincos(ang, &sn, &cs);
-    dst[i] = to_bf16(static_cast<float>(a * cs - c * sn));
-    dst[i + half] = to_bf16(static_cast<float>(a * sn + c * cs));
+    const uint16_t lo = to_bf16(static_cast<float>(a * cs - c * sn));
+    const uint16_t hi = to_bf16(static_cast<float>(a * sn + c * cs));
+    if constexpr (FP4) {
+      if (h >= Hq) {  // uniform over the wavefront
+        store_row4(page4, idx4, tok4, false, i, lo, hi);
+        continue;
+      }
+    }
+    dst[i] = lo;
+    dst[i + half] = hi;
   }
 }
 
@@ -556,8 +621,9 @@ int boost_rope_kv_append_slices(boost_ctx* ctx, const boost_kv_pool* p, int laye
                     static_cast<int>(p->geom.nb)};
   // K = 0: no row of the producing matrix crosses a page
   const Slices sl{qkv, S, B, static_cast<int64_t>(Hq + 2 * H) * D, kPageElems % K ? K : 0};
-  hipLaunchKernelGGL(rope_qkv_kernel<true>,
-                     dim3((B * (Hq + 2 * H) + kRopeWaves - 1) / kRopeWaves),
+  const auto kernel = p->format == BOOST_KV_FP4 ? rope_qkv_kernel<true, true>
+                                                : rope_qkv_kernel<true>;
+  hipLaunchKernelGGL(kernel, dim3((B * (Hq + 2 * H) + kRopeWaves - 1) / kRopeWaves),
                      dim3(64 * kRopeWaves), 0,
                      static_cast<hipStream_t>(stream), sl, positions, Hq, H, D, std::log2(theta),
                      static_cast<uint16_t*>(q), nullptr, nullptr, ps);
@@ -576,6 +642,8 @@ int boost_kv_append(boost_ctx* ctx, const boost_kv_pool* p, int layer,
   if (B < 1 || max_blocks < 1) return fail(BOOST_EINVAL, "B=%d max_blocks=%d", B, max_blocks);
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15)
     return fail(BOOST_EINVAL, "k and v must be 16-byte aligned");
+  if (p->format == BOOST_KV_FP4)
+    return kv_write4(p, layer, nullptr, block_tables, max_blocks, positions, k, v, B, stream);
   const uint64_t P = p->geom.pages;
   const int H = static_cast<int>(p->cfg.kv_heads), D = static_cast<int>(p->cfg.head_dim);
   const int64_t n = static_cast<int64_t>(B) * H * (D / 8);

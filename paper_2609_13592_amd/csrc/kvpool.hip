@@ -1,11 +1,12 @@
 // KV pool (§4.2 LPP, §4.5 heads-outermost layout and two free lists) and the
-// KV write kernel.  Every layer has a K and a V tensor [H][NB][T][D] bf16;
-// the LPP tail pages of each tensor live in pinned host memory, the rest in
+// kernels that write its tokens and read them back.  Every layer has a K and
+// a V tensor [H][NB][T][D], bf16 or in 4 bits (kvfmt.h); the LPP tail pages of each tensor live in pinned host memory, the rest in
 // one HBM slab; the device page table maps (layer, K/V, page) to an address.
 #include <algorithm>
 #include <cstring>
 #include <new>
 
+#include "kvfmt.h"
 #include "runtime.h"
 
 namespace {
@@ -35,6 +36,198 @@ __global__ __launch_bounds__(256) void kv_write_kernel(
   *reinterpret_cast<uint4*>(const_cast<char*>(pt_v[page]) + in) = v[t];
 }
 
+// Reads token slots back: the inverse of kv_write_kernel.
+__global__ __launch_bounds__(256) void kv_read_kernel(
+    const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v,
+    const int32_t* __restrict__ slots, uint4* __restrict__ k, uint4* __restrict__ v, int n, int H,
+    int D, int T, int nb) {
+  const int chunks = D / 8;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (t >= static_cast<int64_t>(n) * H * chunks) return;
+  const int c = static_cast<int>(t % chunks);
+  const int64_t th = t / chunks;
+  const int h = static_cast<int>(th % H);
+  const int32_t slot = slots[th / H];
+  if (slot < 0 || slot >= static_cast<int64_t>(nb) * T) return;
+  const uint64_t byte = ((static_cast<uint64_t>(h) * nb + slot / T) * T + slot % T) * D * 2 +
+                        static_cast<uint64_t>(c) * 16;
+  const uint64_t page = byte >> 21, in = byte & (bst::kPage - 1);
+  k[t] = *reinterpret_cast<const uint4*>(pt_k[page] + in);
+  v[t] = *reinterpret_cast<const uint4*>(pt_v[page] + in);
+}
+
+// ---- 4 bits: one lane per (token, head, group of 32 dims), the four groups
+// of a token in the four lanes of a quad.  Bound by the bytes: 256 in and 68
+// out per row (or the reverse).
+
+template <int K>
+__device__ __forceinline__ uint32_t quad_lane(uint32_t v) {
+  return static_cast<uint32_t>(
+      __builtin_amdgcn_mov_dpp(static_cast<int>(v), K * 0x55, 0xf, 0xf, true));
+}
+
+// Lane c of a quad gets in x[b] lane b's w[c] (a transpose of dwords over the
+// quad).
+__device__ __forceinline__ void quad_transpose(const uint32_t* w, int c, uint32_t* x) {
+  uint32_t a[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i][0] = quad_lane<0>(w[i]);
+    a[i][1] = quad_lane<1>(w[i]);
+    a[i][2] = quad_lane<2>(w[i]);
+    a[i][3] = quad_lane<3>(w[i]);
+  }
+#pragma unroll
+  for (int b = 0; b < 4; ++b) x[b] = c == 0 ? a[0][b] : c == 1 ? a[1][b] : c == 2 ? a[2][b] : a[3][b];
+}
+
+// Byte j of y[i] is byte i of x[j].
+__device__ __forceinline__ void byte_transpose(const uint32_t* x, uint32_t* y) {
+  const uint32_t a0 = __builtin_amdgcn_perm(x[1], x[0], 0x05010400);  // bytes 0, 1 of x0, x1
+  const uint32_t a1 = __builtin_amdgcn_perm(x[3], x[2], 0x05010400);
+  const uint32_t b0 = __builtin_amdgcn_perm(x[1], x[0], 0x07030602);  // bytes 2, 3
+  const uint32_t b1 = __builtin_amdgcn_perm(x[3], x[2], 0x07030602);
+  y[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100);
+  y[1] = __builtin_amdgcn_perm(a1, a0, 0x07060302);
+  y[2] = __builtin_amdgcn_perm(b1, b0, 0x05040100);
+  y[3] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
+}
+
+// 32 bf16 values (64 bytes at src) as floats, and their scale byte.
+__device__ __forceinline__ uint32_t load_group(const uint4* src, float* f) {
+  uint32_t amax = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint4 u = src[i];
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      amax = max(amax, max((w[j] << 16) & 0x7fff0000u, w[j] & 0x7fff0000u));
+      f[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
+      f[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    }
+  }
+  return bst::fp4_scale_byte(amax);
+}
+
+// Slot of row i: given (slots), or that of request i's token at pos[i] (a
+// position or a block outside the table or the pool: -1).
+struct RowSlot {
+  const int32_t* slots;
+  const int32_t* tables;
+  const int32_t* pos;
+  int max_blocks;
+};
+__device__ __forceinline__ int64_t slot_of(const RowSlot& r, int64_t i, int nb) {
+  int64_t slot;
+  if (r.slots) {
+    slot = r.slots[i];
+  } else {
+    const int p = r.pos[i];
+    if (p < 0 || p / bst::kFp4Tok >= r.max_blocks) return -1;
+    const int32_t blk = r.tables[i * r.max_blocks + p / bst::kFp4Tok];
+    if (blk < 0) return -1;
+    slot = static_cast<int64_t>(blk) * bst::kFp4Tok + p % bst::kFp4Tok;
+  }
+  return slot < static_cast<int64_t>(nb) * bst::kFp4Tok ? slot : -1;
+}
+
+__global__ __launch_bounds__(256) void kv_write4_kernel(
+    const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v, RowSlot rows,
+    const uint4* __restrict__ k, const uint4* __restrict__ v, int n, int H, int nb) {
+  using namespace bst;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (t >= static_cast<int64_t>(n) * H * 4) return;  // whole quads
+  const int g = static_cast<int>(t & 3);
+  const int64_t th = t >> 2;
+  const int h = static_cast<int>(th % H);
+  const int64_t slot = slot_of(rows, th / H, nb);
+  if (slot < 0) return;
+  const int tok = static_cast<int>(slot % kFp4Tok);
+  const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
+  char* const pk = const_cast<char*>(pt_k[at.page]);
+  char* const pv = const_cast<char*>(pt_v[at.page]);
+  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale + tok * 4 + g;
+  float f[32];
+  uint32_t sb = load_group(k + t * 4, f);
+  float s = fp4_scale(sb);
+  uint32_t w[4], x[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // dims 8 i .. 8 i + 7 of the group
+    w[i] = fp4_pack<0>(0u, f[8 * i], f[8 * i + 1], s);
+    w[i] = fp4_pack<1>(w[i], f[8 * i + 2], f[8 * i + 3], s);
+    w[i] = fp4_pack<2>(w[i], f[8 * i + 4], f[8 * i + 5], s);
+    w[i] = fp4_pack<3>(w[i], f[8 * i + 6], f[8 * i + 7], s);
+  }
+  *reinterpret_cast<uint4*>(pk + code + tok * 64 + g * 16) = make_uint4(w[0], w[1], w[2], w[3]);
+  pk[scale] = static_cast<char>(sb);
+  sb = load_group(v + t * 4, f);
+  s = fp4_scale(sb);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // bytes r = 4 i .. 4 i + 3: dims r and 16 + r of the group
+    w[i] = fp4_pack<0>(0u, f[4 * i], f[16 + 4 * i], s);
+    w[i] = fp4_pack<1>(w[i], f[4 * i + 1], f[16 + 4 * i + 1], s);
+    w[i] = fp4_pack<2>(w[i], f[4 * i + 2], f[16 + 4 * i + 2], s);
+    w[i] = fp4_pack<3>(w[i], f[4 * i + 3], f[16 + 4 * i + 3], s);
+  }
+  // lane g's dwords are rows r = 4 g .. 4 g + 3 of every group
+  quad_transpose(w, g, x);
+  byte_transpose(x, w);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    *reinterpret_cast<uint32_t*>(pv + code + (tok / 4) * 256 + (4 * g + i) * 16 + (tok % 4) * 4) =
+        w[i];
+  pv[scale] = static_cast<char>(sb);
+}
+
+__global__ __launch_bounds__(256) void kv_read4_kernel(
+    const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v,
+    const int32_t* __restrict__ slots, uint4* __restrict__ k, uint4* __restrict__ v, int n, int H,
+    int nb) {
+  using namespace bst;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+  if (t >= static_cast<int64_t>(n) * H * 4) return;
+  const int g = static_cast<int>(t & 3);
+  const int64_t th = t >> 2;
+  const int h = static_cast<int>(th % H);
+  const int64_t slot = slot_of(RowSlot{slots, nullptr, nullptr, 0}, th / H, nb);
+  if (slot < 0) return;
+  const int tok = static_cast<int>(slot % kFp4Tok);
+  const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
+  const char* const pk = pt_k[at.page];
+  const char* const pv = pt_v[at.page];
+  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale + tok * 4 + g;
+  const uint4 u = *reinterpret_cast<const uint4*>(pk + code + tok * 64 + g * 16);
+  uint32_t x[4], w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    x[i] = *reinterpret_cast<const uint32_t*>(pv + code + (tok / 4) * 256 + (4 * g + i) * 16 +
+                                              (tok % 4) * 4);
+  const float sk = fp4_scale(static_cast<uint8_t>(pk[scale]));
+  const float sv = fp4_scale(static_cast<uint8_t>(pv[scale]));
+  const uint32_t c[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    k[t * 4 + i] = make_uint4(fp4_unpack<0>(c[i], sk), fp4_unpack<1>(c[i], sk),
+                              fp4_unpack<2>(c[i], sk), fp4_unpack<3>(c[i], sk));
+  byte_transpose(x, w);      // w[b]: rows 4 g .. 4 g + 3 of group b
+  quad_transpose(w, g, x);   // x[i]: rows 4 i .. 4 i + 3 of this lane's group
+  uint32_t lo[8], hi[8];     // dims 2 i, 2 i + 1 and 16 + 2 i, 16 + 2 i + 1
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = fp4_unpack<0>(x[i], sv), b = fp4_unpack<1>(x[i], sv);
+    const uint32_t d = fp4_unpack<2>(x[i], sv), e = fp4_unpack<3>(x[i], sv);
+    lo[2 * i] = __builtin_amdgcn_perm(b, a, 0x05040100);
+    hi[2 * i] = __builtin_amdgcn_perm(b, a, 0x07060302);
+    lo[2 * i + 1] = __builtin_amdgcn_perm(e, d, 0x05040100);
+    hi[2 * i + 1] = __builtin_amdgcn_perm(e, d, 0x07060302);
+  }
+  v[t * 4] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  v[t * 4 + 1] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
+  v[t * 4 + 2] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  v[t * 4 + 3] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+}
+
 int destroy(boost_kv_pool* p) {
   if (!p) return BOOST_OK;
   if (p->ctx && p->ctx->device >= 0) (void)hipSetDevice(p->ctx->device);
@@ -54,6 +247,31 @@ int kv_parts_for(const boost_kv_pool* p, int max_blocks) {
   const int tokens = max_blocks * static_cast<int>(p->cfg.block_tokens);
   return std::max(1, (tokens + kPartTokensMin - 1) / kPartTokensMin);
 }
+
+int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv) {
+  if (p->ctx->device < 0 || !p->d_page_table) return fail(BOOST_ENODEV, "plan-only pool");
+  if (layer < 0 || static_cast<uint32_t>(layer) >= p->cfg.layers)
+    return fail(BOOST_EINVAL, "layer %d", layer);
+  *pk = p->d_page_table + (2ull * layer) * p->geom.pages;
+  *pv = p->d_page_table + (2ull * layer + 1) * p->geom.pages;
+  return BOOST_OK;
+}
+
+int kv_write4(const boost_kv_pool* p, int layer, const int32_t* slots, const int32_t* tables,
+              int max_blocks, const int32_t* positions, const void* k, const void* v, int n,
+              void* stream) {
+  const char* const *pk, * const *pv;
+  if (int rc = kv_layer(p, layer, &pk, &pv)) return rc;
+  const int H = static_cast<int>(p->cfg.kv_heads);
+  const int64_t grid = (static_cast<int64_t>(n) * H * 4 + 255) / 256;
+  if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "n=%d: grid too large", n);
+  hipLaunchKernelGGL(kv_write4_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
+                     static_cast<hipStream_t>(stream), pk, pv,
+                     RowSlot{slots, tables, positions, max_blocks}, static_cast<const uint4*>(k),
+                     static_cast<const uint4*>(v), n, H, static_cast<int>(p->geom.nb));
+  BOOST_HIP(hipGetLastError());
+  return BOOST_OK;
+}
 }  // namespace bst
 
 using namespace bst;
@@ -61,8 +279,17 @@ using namespace bst;
 extern "C" {
 
 int boost_kv_pool_create(boost_ctx* ctx, const boost_kv_cfg* cfg, boost_kv_pool** out) {
+  return boost_kv_pool_create_format(ctx, cfg, BOOST_KV_BF16, out);
+}
+
+int boost_kv_pool_create_format(boost_ctx* ctx, const boost_kv_cfg* cfg, int format,
+                                boost_kv_pool** out) {
   if (!ctx || !cfg || !out) return fail(BOOST_EINVAL, "null argument");
   *out = nullptr;
+  if (format != BOOST_KV_BF16 && format != BOOST_KV_FP4)
+    return fail(BOOST_EINVAL, "format %d", format);
+  if (format == BOOST_KV_FP4 && cfg->head_dim != static_cast<uint32_t>(kFp4D))
+    return fail(BOOST_EINVAL, "a 4-bit pool needs head_dim %d", kFp4D);
   if (cfg->layers == 0) return fail(BOOST_EINVAL, "0 layers");
   if (cfg->block_tokens != 16) return fail(BOOST_EINVAL, "block_tokens must be 16");
   if (cfg->head_dim != 64 && cfg->head_dim != 128)
@@ -77,8 +304,10 @@ int boost_kv_pool_create(boost_ctx* ctx, const boost_kv_cfg* cfg, boost_kv_pool*
     p = new boost_kv_pool();
     p->ctx = ctx;
     p->cfg = *cfg;
+    p->format = format;
     int rc = kv_geometry(cfg->n_blocks, cfg->kv_heads, cfg->head_dim, cfg->block_tokens,
-                         cfg->M, cfg->tier_mode, cfg->layers, cfg->hbm_budget_bytes, p->geom);
+                         cfg->M, cfg->tier_mode, cfg->layers, cfg->hbm_budget_bytes,
+                         format == BOOST_KV_FP4 ? kFp4Page : 0, p->geom);
     if (rc) {
       delete p;
       return rc;
@@ -159,6 +388,27 @@ int boost_kv_pool_info(const boost_kv_pool* p, boost_kv_info* info) {
 
 int boost_kv_pool_destroy(boost_kv_pool* p) { return destroy(p); }
 
+int boost_kv_pool_format(const boost_kv_pool* p, int* format) {
+  if (!p || !format) return fail(BOOST_EINVAL, "null argument");
+  *format = p->format;
+  return BOOST_OK;
+}
+
+int boost_kv_pages(const boost_kv_pool* p, int layer, int which, uint64_t* addresses,
+                   uint64_t cap, uint64_t* n_pages) {
+  if (!p || !n_pages || (cap && !addresses)) return fail(BOOST_EINVAL, "null argument");
+  if (p->ctx->device < 0) return fail(BOOST_ENODEV, "plan-only pool");
+  if (layer < 0 || static_cast<uint32_t>(layer) >= p->cfg.layers || which < 0 || which > 1)
+    return fail(BOOST_EINVAL, "layer %d, tensor %d", layer, which);
+  const uint64_t P = p->geom.pages, Hp = p->geom.host_pages, t = 2ull * layer + which;
+  *n_pages = P;
+  for (uint64_t pg = 0; pg < std::min(P, cap); ++pg)
+    addresses[pg] = reinterpret_cast<uint64_t>(
+        pg < P - Hp ? p->hbm.base + (t * (P - Hp) + pg) * kPage
+                    : p->host[layer].base + (which * Hp + (pg - (P - Hp))) * kPage);
+  return BOOST_OK;
+}
+
 int boost_kv_block_host_heads(const boost_kv_pool* p, int32_t block, uint32_t* n) {
   if (!p || !n) return fail(BOOST_EINVAL, "null argument");
   if (block < 0 || static_cast<uint32_t>(block) >= p->geom.nb)
@@ -203,6 +453,8 @@ int boost_kv_write(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int3
   if (n == 0) return BOOST_OK;
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15)
     return fail(BOOST_EINVAL, "k and v must be 16-byte aligned");
+  if (p->format == BOOST_KV_FP4)
+    return kv_write4(p, layer, slots, nullptr, 0, nullptr, k, v, n, stream);
   const uint64_t P = p->geom.pages;
   const char* const* pk = p->d_page_table + (2ull * layer) * P;
   const char* const* pv = p->d_page_table + (2ull * layer + 1) * P;
@@ -212,6 +464,32 @@ int boost_kv_write(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int3
                      static_cast<const uint4*>(k), static_cast<const uint4*>(v), n,
                      static_cast<int>(p->cfg.kv_heads), static_cast<int>(p->cfg.head_dim),
                      static_cast<int>(p->cfg.block_tokens), static_cast<int>(p->geom.nb));
+  BOOST_HIP(hipGetLastError());
+  return BOOST_OK;
+}
+
+int boost_kv_read(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int32_t* slots, void* k,
+                  void* v, int n, void* stream) {
+  if (!ctx || !p || !slots || !k || !v) return fail(BOOST_EINVAL, "null argument");
+  const char* const *pk, * const *pv;
+  if (int rc = kv_layer(p, layer, &pk, &pv)) return rc;
+  if (n < 0) return fail(BOOST_EINVAL, "n=%d", n);
+  if (n == 0) return BOOST_OK;
+  if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15)
+    return fail(BOOST_EINVAL, "k and v must be 16-byte aligned");
+  const int H = static_cast<int>(p->cfg.kv_heads), D = static_cast<int>(p->cfg.head_dim);
+  const bool fp4 = p->format == BOOST_KV_FP4;
+  const int64_t grid = (static_cast<int64_t>(n) * H * (fp4 ? 4 : D / 8) + 255) / 256;
+  if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "n=%d: grid too large", n);
+  const dim3 g(static_cast<unsigned>(grid));
+  const auto s = static_cast<hipStream_t>(stream);
+  if (fp4)
+    hipLaunchKernelGGL(kv_read4_kernel, g, dim3(256), 0, s, pk, pv, slots, static_cast<uint4*>(k),
+                       static_cast<uint4*>(v), n, H, static_cast<int>(p->geom.nb));
+  else
+    hipLaunchKernelGGL(kv_read_kernel, g, dim3(256), 0, s, pk, pv, slots, static_cast<uint4*>(k),
+                       static_cast<uint4*>(v), n, H, D, static_cast<int>(p->cfg.block_tokens),
+                       static_cast<int>(p->geom.nb));
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

@@ -84,6 +84,7 @@ constexpr uint64_t kGemmWsFloats = 16ull << 20;  // split-K workspace per contex
 struct boost_kv_pool {
   boost_ctx* ctx = nullptr;
   boost_kv_cfg cfg{};
+  int format = BOOST_KV_BF16;
   bst::KvGeom geom;
   bst::Dsr dsr;
   // device backing (absent on a plan-only context)
@@ -94,3 +95,16 @@ struct boost_kv_pool {
   float* d_part_ml = nullptr;     // [max_batch][q_heads][max_parts][2] (max, sum)
   int max_parts = 0;
 };
+
+namespace bst {
+
+// Page tables of one layer's K and V (ENODEV: plan-only pool, EINVAL: layer).
+int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv);
+
+// n rows [H, 128] of K and V into a 4-bit pool, at the given slots or (slots
+// null) at the requests' positions; arguments checked by the caller.
+int kv_write4(const boost_kv_pool* p, int layer, const int32_t* slots, const int32_t* tables,
+              int max_blocks, const int32_t* positions, const void* k, const void* v, int n,
+              void* stream);
+
+}  // namespace bst
