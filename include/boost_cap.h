@@ -577,6 +577,70 @@ int boost_paged_attn_decode_noalloc(boost_ctx *ctx, const boost_kv_pool *pool,
                                     const int32_t *ctx_lens, float scale,
                                     void *out, int out_dtype, void *stream);
 
+/* ------------------------------------- sparse attention over a long context */
+
+/* A decode step of a long context that reads a part of it: every block has a
+ * summary of its keys in HBM, a cheap score of the query against the
+ * summaries selects blocks for each KV head, and attention runs over those.
+ * All three calls are asynchronous on `stream`, allocate nothing and may be
+ * captured; they are ordered like other calls on the pool (a summary is read
+ * after the update that wrote it). */
+
+/* Give the pool room for the summaries: 257 bytes of HBM per layer, KV head
+ * and block, beside what tier_mode places (zero at first: score 0).  Freed
+ * with the pool; again is a no-op.  Synchronises.  head_dim 128.
+ * Errors: EINVAL, ENODEV, ENOMEM, EHIP. */
+int boost_kv_index_enable(boost_kv_pool *pool);
+
+/* Summarise the blocks of one layer that hold tokens [starts[b], ends[b]) of
+ * every request, each over all of its tokens below ends[b]: after a prompt
+ * from 0, in a decode step from the new token's position.  For each dim the
+ * largest and the smallest key, in whole steps of 2^e rounded outwards to 8
+ * bits, e the smallest in [-126, 122] with max|k| <= 127 * 2^e.  Blocks outside
+ * the table or the pool are skipped; a block with an infinity or a NaN among
+ * its keys scores +inf.  starts, ends: device int32 [B].  max_tokens is the
+ * largest ends - starts (it sizes the launch; larger ranges are done all the
+ * same).  Two requests must not update the same block in one call with other
+ * ends.  Errors: EINVAL (also: no summaries), ENODEV, EHIP. */
+int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
+                          const int32_t *block_tables, int max_blocks,
+                          const int32_t *starts, const int32_t *ends, int B,
+                          int max_tokens, void *stream);
+
+/* The blocks that request b's query heads of KV head g read.  With q8 the
+ * query in whole steps of 2^eq (rounded to nearest, ties to even, eq chosen
+ * like e), a block's score is
+ *   max over the KV head's query heads of 2^(e + eq) sum_d max(q8 hi, q8 lo),
+ * an upper bound of q8 . k; the sum is one of whole numbers, so scores are
+ * exact and the selection is reproducible on every placement.  A query head
+ * that is not finite counts as 0, a block outside the pool as -inf.
+ * With n = ceil(ctx_lens[b] / T) blocks (at most max_blocks), the first
+ * n_first and the last n_last of them are taken always, then those with the
+ * largest scores, ties to the lowest index, top_k in all (all n when n <=
+ * top_k).  scores: device fp32 [B, H, max_blocks], caller-owned; entries past
+ * a request's blocks are left as they are.  sel: device int32 [B, H, top_k]:
+ * indices of blocks in the context, ascending, then -1.
+ * q: device bf16 [B, Hq, 128], 16-byte aligned, Hq / H up to 16.
+ * n_first + n_last <= top_k.  Errors: EINVAL, ENODEV, EHIP. */
+int boost_kv_select(boost_ctx *ctx, const boost_kv_pool *pool, int layer, const void *q,
+                    int B, int Hq, const int32_t *block_tables, int max_blocks,
+                    const int32_t *ctx_lens, int top_k, int n_first, int n_last,
+                    float *scores, int32_t *sel, void *stream);
+
+/* boost_paged_attn_decode over the blocks that sel names for each KV head in
+ * place of the whole context: the softmax runs over their tokens below
+ * ctx_lens[b].  Of a list the first min(top_k, ceil(ctx_lens[b] / T)) entries
+ * count, in any order; an entry that names no block of the context (-1, or
+ * past it) is skipped, one that comes twice counts twice.  A list with every
+ * block gives boost_paged_attn_decode's result up to rounding.
+ * sel: device int32 [B, H, top_k].  Other arguments, scratch and errors as
+ * boost_paged_attn_decode; EINVAL for top_k < 1. */
+int boost_sparse_attn_decode(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
+                             const void *q, int B, int Hq, const int32_t *block_tables,
+                             int max_blocks, const int32_t *ctx_lens, const int32_t *sel,
+                             int top_k, float scale, void *out, int out_dtype,
+                             void *stream);
+
 /* -------------------------------------------- a6: glue of a full decode step */
 
 /* The paper measures whole decode steps of Llama-style models (§5.1) without

@@ -50,7 +50,7 @@ def stored(u16: np.ndarray) -> np.ndarray:
     """What bf16 values [..., D] (raw bits, D a multiple of 32) read back as
     from a 4-bit pool, in fp64."""
     x = bf16_to_f32(u16).astype(np.float64)
-    g = x.reshape(*x.shape[:-1], -1, 32)
+    g = x.reshape(*x.shape[:-1], x.shape[-1] // 32, 32)
     bad = ~np.isfinite(g).all(-1, keepdims=True)
     g = np.where(bad, 0.0, g)
     s = np.ldexp(1.0, exponents_fast(g))[..., None]

@@ -124,6 +124,12 @@ _SIGS = {
                                        _vp, C.c_float, _vp, _i32, _vp]),
     "boost_paged_attn_decode_noalloc": (_i32, [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32,
                                                _vp, C.c_float, _vp, _i32, _vp]),
+    "boost_kv_index_enable": (_i32, [_vp]),
+    "boost_kv_index_update": (_i32, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp]),
+    "boost_kv_select": (_i32, [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _i32, _i32,
+                               _i32, _vp, _vp, _vp]),
+    "boost_sparse_attn_decode": (_i32, [_vp, _vp, _i32, _vp, _i32, _i32, _vp, _i32, _vp, _vp,
+                                        _i32, C.c_float, _vp, _i32, _vp]),
     "boost_decode_gemv": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _i32, _vp]),
     "boost_decode_gemv_slices": (_i32, [_vp, _vp, _i32, _i32, _vp, _i32, _vp, _i32,
                                         C.POINTER(_i32), _vp]),
@@ -526,6 +532,35 @@ def boost_paged_attn_decode_noalloc(ctx: int, pool: int, layer: int, q, B: int, 
                                                   _ptr(block_tables), max_blocks,
                                                   _ptr(ctx_lens), scale, _ptr(out),
                                                   out_dtype, _stream(stream)))
+
+
+# ----------------------------------------------------------- sparse attention
+def boost_kv_index_enable(pool: int):
+    _check(load().boost_kv_index_enable(pool))
+
+
+def boost_kv_index_update(ctx: int, pool: int, layer: int, block_tables, max_blocks: int,
+                          starts, ends, B: int, max_tokens: int, stream=None):
+    _check(load().boost_kv_index_update(ctx, pool, layer, _ptr(block_tables), max_blocks,
+                                        _ptr(starts), _ptr(ends), B, max_tokens,
+                                        _stream(stream)))
+
+
+def boost_kv_select(ctx: int, pool: int, layer: int, q, B: int, Hq: int, block_tables,
+                    max_blocks: int, ctx_lens, top_k: int, n_first: int, n_last: int,
+                    scores, sel, stream=None):
+    _check(load().boost_kv_select(ctx, pool, layer, _ptr(q), B, Hq, _ptr(block_tables),
+                                  max_blocks, _ptr(ctx_lens), top_k, n_first, n_last,
+                                  _ptr(scores), _ptr(sel), _stream(stream)))
+
+
+def boost_sparse_attn_decode(ctx: int, pool: int, layer: int, q, B: int, Hq: int,
+                             block_tables, max_blocks: int, ctx_lens, sel, top_k: int,
+                             scale: float, out, out_dtype: int = DTYPE_F32, stream=None):
+    _check(load().boost_sparse_attn_decode(ctx, pool, layer, _ptr(q), B, Hq,
+                                           _ptr(block_tables), max_blocks, _ptr(ctx_lens),
+                                           _ptr(sel), top_k, scale, _ptr(out), out_dtype,
+                                           _stream(stream)))
 
 
 # ---------------------------------------------------------- decode-step glue

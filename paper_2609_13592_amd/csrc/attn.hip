@@ -132,6 +132,12 @@ __device__ __forceinline__ void slot_merge(float* m, float* l, float (*acc)[8]) 
   merge_state<G>(m, l, acc, m2, l2, a2);
 }
 
+// V of a token that does not count: zeros, whatever its slot holds (its
+// probability 0 must not meet an infinity or a NaN there).
+__device__ __forceinline__ uint4 live(const uint4& v, bool valid) {
+  return make_uint4(valid ? v.x : 0, valid ? v.y : 0, valid ? v.z : 0, valid ? v.w : 0);
+}
+
 // Online-softmax update of one token slot with U blocks.  Scores are in the
 // log2 domain (q . k * scale * log2 e), so exp2 is one instruction.  With
 // MASKED false every token is valid; otherwise invalid tokens have score -inf
@@ -168,7 +174,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float vf[8];
-    unpack8(vb[u], vf);
+    unpack8(MASKED ? live(vb[u], valid[u]) : vb[u], vf);
 #pragma unroll
     for (int j = 0; j < G; ++j) {
       // masked: an invalid token (score -inf) weighs 0, also while the
@@ -292,7 +298,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
       lh[i] += p[i];
     }
     bcast_groups<G>(p, pj);
-    unpack8(vb[u], vf);
+    unpack8(MASKED ? live(vb[u], valid[u]) : vb[u], vf);
 #pragma unroll
     for (int j = 0; j < G; ++j)
 #pragma unroll

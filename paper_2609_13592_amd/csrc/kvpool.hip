@@ -234,6 +234,7 @@ int destroy(boost_kv_pool* p) {
   (void)hipFree(p->d_page_table);
   (void)hipFree(p->d_part_acc);
   (void)hipFree(p->d_part_ml);
+  (void)hipFree(p->d_index);
   bst::slab_free(p->hbm);
   for (auto& h : p->host) bst::slab_free(h);
   delete p;

@@ -94,6 +94,9 @@ struct boost_kv_pool {
   float* d_part_acc = nullptr;    // [max_batch][q_heads][max_parts][D]
   float* d_part_ml = nullptr;     // [max_batch][q_heads][max_parts][2] (max, sum)
   int max_parts = 0;
+  // block summaries (boost_kv_index_enable): [layers][H][nb][256], then the
+  // exponents [layers][H][nb]
+  int8_t* d_index = nullptr;
 };
 
 namespace bst {
