@@ -434,7 +434,7 @@ typedef struct boost_kv_info {
 
 typedef struct boost_kv_usage {
   uint32_t free_shh, free_local;  /* free blocks on each list */
-  uint64_t used_blocks;           /* blocks held by requests */
+  uint64_t used_blocks;           /* blocks held by requests (a shared one once) */
   uint64_t used_host_head_blocks; /* sum of host heads over held blocks */
   uint32_t requests, shh_requests;
 } boost_kv_usage;
@@ -506,9 +506,60 @@ int boost_kv_block_host_heads(const boost_kv_pool *pool, int32_t block,
 int boost_kv_alloc(boost_kv_pool *pool, uint64_t request_id, uint32_t n_blocks,
                    int32_t *block_ids_out);
 
-/* Return every block of the request to its list and forget the request.
+/* Return every block of the request to its list (one that other requests hold
+ * too stays theirs) and forget the request.
  * Errors: EINVAL (unknown request). */
 int boost_kv_free(boost_kv_pool *pool, uint64_t request_id);
+
+/* Requests that share blocks (a common prompt, several answers to one), and
+ * blocks that are given back or moved while a request lives.  The paper's
+ * allocator hands blocks out and takes a request's back; these keep its two
+ * lists, types and order.  CPU only; what a block holds is copied by
+ * boost_kv_copy_blocks.
+ *
+ * boost_kv_fork: a new request `child` of the parent's type that holds the
+ * parent's first n_blocks blocks with it.  Shared blocks are read by both and
+ * written by neither.  Errors: EINVAL (unknown parent, child exists, n_blocks 0
+ * or more than the parent holds), ENOMEM.
+ *
+ * boost_kv_unshare: before the request writes into its index-th block.  Held by
+ * it alone: *src = *dst = the block.  Shared: the request gets a free block
+ * *dst in its place, as boost_kv_alloc hands one out, and the caller copies
+ * *src to it.  Errors: EINVAL (unknown request, index), EAGAIN (no free block;
+ * nothing changes).
+ *
+ * boost_kv_truncate: the request keeps its first n_keep blocks (0 too: it stays
+ * live) and gives the others back.  Errors: EINVAL, ENOMEM.
+ *
+ * boost_kv_compact: moves held blocks to free ones of the same list with lower
+ * ids, at most max_moves of them, the highest first, until the held blocks of
+ * each list are its lowest: the rest of the pool can then be left out of a copy
+ * or a snapshot of it.  Writes *n_moves pairs (src, dst), every src and dst
+ * once; all holders are renamed.  The caller copies the pairs in one call,
+ * before anything else is written to the pool, and rebuilds its block tables
+ * (boost_kv_request_blocks).  Errors: EINVAL, ENOMEM.
+ *
+ * boost_kv_request_blocks: the request's blocks in order, min(count, cap) of
+ * them (blocks may be NULL with cap 0), the count to *n.  Errors: EINVAL. */
+int boost_kv_fork(boost_kv_pool *pool, uint64_t parent, uint64_t child, uint32_t n_blocks);
+int boost_kv_unshare(boost_kv_pool *pool, uint64_t request_id, uint32_t index, int32_t *src,
+                     int32_t *dst);
+int boost_kv_truncate(boost_kv_pool *pool, uint64_t request_id, uint32_t n_keep);
+int boost_kv_compact(boost_kv_pool *pool, uint32_t max_moves, int32_t *src, int32_t *dst,
+                     uint32_t *n_moves);
+int boost_kv_request_blocks(const boost_kv_pool *pool, uint64_t request_id, int32_t *blocks,
+                            uint32_t cap, uint32_t *n);
+
+/* Copy block src[i] to block dst[i], i < n, in layers [layer0, layer0 +
+ * n_layers): keys and values of every KV head, on whichever tier they lie, and
+ * the blocks' summaries where the pool has them.  src, dst: HOST arrays, read
+ * before the call returns.  A source may serve several destinations; a
+ * destination comes once and is no source.  n = 0 does nothing.  Asynchronous
+ * on `stream`; may be captured (a graph keeps the pairs of its capture).
+ * Errors: EINVAL (layers, a block outside the pool, a destination twice or
+ * among the sources), ENODEV, ENOMEM, EHIP. */
+int boost_kv_copy_blocks(boost_ctx *ctx, const boost_kv_pool *pool, int layer0, int n_layers,
+                         const int32_t *src, const int32_t *dst, int n, void *stream);
 
 /* Current type (BOOST_KV_LOCAL / BOOST_KV_SHH) of a live request. */
 int boost_kv_request_type(const boost_kv_pool *pool, uint64_t request_id,

@@ -117,6 +117,12 @@ _SIGS = {
     "boost_kv_block_host_heads": (_i32, [_vp, C.c_int32, C.POINTER(_u32)]),
     "boost_kv_alloc": (_i32, [_vp, _u64, _u32, _vp]),
     "boost_kv_free": (_i32, [_vp, _u64]),
+    "boost_kv_fork": (_i32, [_vp, _u64, _u64, _u32]),
+    "boost_kv_unshare": (_i32, [_vp, _u64, _u32, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]),
+    "boost_kv_truncate": (_i32, [_vp, _u64, _u32]),
+    "boost_kv_compact": (_i32, [_vp, _u32, _vp, _vp, C.POINTER(_u32)]),
+    "boost_kv_request_blocks": (_i32, [_vp, _u64, _vp, _u32, C.POINTER(_u32)]),
+    "boost_kv_copy_blocks": (_i32, [_vp, _vp, _i32, _i32, _vp, _vp, _i32, _vp]),
     "boost_kv_request_type": (_i32, [_vp, _u64, C.POINTER(_i32)]),
     "boost_kv_stats": (_i32, [_vp, C.POINTER(KVStats)]),
     "boost_kv_write": (_i32, [_vp, _vp, _i32, _vp, _vp, _vp, _i32, _vp]),
@@ -492,6 +498,52 @@ def boost_kv_alloc(pool: int, request_id: int, n_blocks: int):
 
 def boost_kv_free(pool: int, request_id: int):
     _check(load().boost_kv_free(pool, request_id))
+
+
+def boost_kv_fork(pool: int, parent: int, child: int, n_blocks: int):
+    _check(load().boost_kv_fork(pool, parent, child, n_blocks))
+
+
+def boost_kv_unshare(pool: int, request_id: int, index: int):
+    """(src, dst) of the block, equal when it is the request's alone, or EAGAIN
+    (the int) when the pool has no free block."""
+    s, d = C.c_int32(), C.c_int32()
+    rc = load().boost_kv_unshare(pool, request_id, index, C.byref(s), C.byref(d))
+    if rc == EAGAIN:
+        return EAGAIN
+    _check(rc)
+    return s.value, d.value
+
+
+def boost_kv_truncate(pool: int, request_id: int, n_keep: int):
+    _check(load().boost_kv_truncate(pool, request_id, n_keep))
+
+
+def boost_kv_compact(pool: int, max_moves: int):
+    """The moves as two arrays (src, dst)."""
+    src, dst = np.zeros((2, max(max_moves, 1)), dtype=np.int32)
+    n = _u32()
+    _check(load().boost_kv_compact(pool, max_moves, _ptr(src), _ptr(dst), C.byref(n)))
+    return src[:n.value], dst[:n.value]
+
+
+def boost_kv_request_blocks(pool: int, request_id: int) -> np.ndarray:
+    n = _u32()
+    _check(load().boost_kv_request_blocks(pool, request_id, None, 0, C.byref(n)))
+    out = np.zeros(n.value, dtype=np.int32)
+    _check(load().boost_kv_request_blocks(pool, request_id, _ptr(out), out.size, C.byref(n)))
+    return out
+
+
+def boost_kv_copy_blocks(ctx: int, pool: int, layer0: int, n_layers: int, src, dst, n: int,
+                         stream=None):
+    """src, dst: block ids on the host."""
+    s = np.ascontiguousarray(src, dtype=np.int32)
+    d = np.ascontiguousarray(dst, dtype=np.int32)
+    if min(s.size, d.size) < n:
+        raise ValueError(f"{n} pairs needed, {min(s.size, d.size)} given")
+    _check(load().boost_kv_copy_blocks(ctx, pool, layer0, n_layers, _ptr(s), _ptr(d), n,
+                                       _stream(stream)))
 
 
 def boost_kv_request_type(pool: int, request_id: int) -> int:

@@ -62,6 +62,7 @@ void Dsr::init(const KvGeom& g) {
   free_[1].clear();
   req_.clear();
   is_shh_.assign(g.nb, 0);
+  refs_.assign(g.nb, 0);
   host_heads_ = g.host_heads;
   for (uint32_t b = 0; b < g.nb; ++b) {
     const bool shh = g.hi != g.lo && g.host_heads[b] == g.hi;
@@ -90,32 +91,135 @@ int Dsr::alloc(uint64_t rid, uint32_t n, int32_t* out) {
       type = BOOST_KV_LOCAL;
     else
       type = BOOST_KV_SHH;
-    it = req_.emplace(rid, Req{type, {}}).first;
+    Req fresh{type, {}};
+    fresh.blocks.reserve(n);  // nothing changes if there is no memory for it
+    it = req_.emplace(rid, std::move(fresh)).first;
   }
   Req& r = it->second;
+  r.blocks.reserve(r.blocks.size() + n);
   for (uint32_t i = 0; i < n; ++i) {
-    if (free_[r.type].empty()) r.type ^= 1;  // sticky switch to the other list
-    auto first = free_[r.type].begin();
-    const int32_t b = *first;
-    free_[r.type].erase(first);
-    r.blocks.push_back(b);
-    out[i] = b;
-    used_ += 1;
-    used_hh_ += host_heads_[b];
+    out[i] = take(r);
+    r.blocks.push_back(out[i]);
   }
   return BOOST_OK;
+}
+
+int32_t Dsr::take(Req& r) {
+  if (free_[r.type].empty()) r.type ^= 1;  // sticky switch to the other list
+  auto first = free_[r.type].begin();
+  const int32_t b = *first;
+  free_[r.type].erase(first);
+  refs_[b] = 1;
+  used_ += 1;
+  used_hh_ += host_heads_[b];
+  return b;
+}
+
+void Dsr::drop(int32_t b) {
+  if (refs_[b] > 1) {
+    refs_[b] -= 1;
+    return;
+  }
+  free_[is_shh_[b] ? BOOST_KV_SHH : BOOST_KV_LOCAL].insert(b);
+  refs_[b] = 0;
+  used_ -= 1;
+  used_hh_ -= host_heads_[b];
 }
 
 int Dsr::release(uint64_t rid) {
   auto it = req_.find(rid);
   if (it == req_.end())
     return fail(BOOST_EINVAL, "unknown request %llu", (unsigned long long)rid);
-  for (int32_t b : it->second.blocks) {
-    free_[is_shh_[b] ? BOOST_KV_SHH : BOOST_KV_LOCAL].insert(b);
-    used_ -= 1;
-    used_hh_ -= host_heads_[b];
-  }
+  for (auto& held = it->second.blocks; !held.empty(); held.pop_back()) drop(held.back());
   req_.erase(it);
+  return BOOST_OK;
+}
+
+int Dsr::fork(uint64_t parent, uint64_t child, uint32_t n) {
+  auto it = req_.find(parent);
+  if (it == req_.end())
+    return fail(BOOST_EINVAL, "unknown request %llu", (unsigned long long)parent);
+  if (req_.count(child))
+    return fail(BOOST_EINVAL, "request %llu exists", (unsigned long long)child);
+  const std::vector<int32_t>& held = it->second.blocks;
+  if (n == 0 || n > held.size())
+    return fail(BOOST_EINVAL, "%u blocks of a request that holds %zu", n, held.size());
+  Req r{it->second.type, std::vector<int32_t>(held.begin(), held.begin() + n)};
+  const Req& c = req_.emplace(child, std::move(r)).first->second;
+  for (int32_t b : c.blocks) refs_[b] += 1;
+  return BOOST_OK;
+}
+
+int Dsr::unshare(uint64_t rid, uint32_t index, int32_t* src, int32_t* dst) {
+  auto it = req_.find(rid);
+  if (it == req_.end() || !src || !dst)
+    return fail(BOOST_EINVAL, "unknown request %llu", (unsigned long long)rid);
+  Req& r = it->second;
+  if (index >= r.blocks.size())
+    return fail(BOOST_EINVAL, "block %u of a request that holds %zu", index, r.blocks.size());
+  const int32_t b = r.blocks[index];
+  if (refs_[b] > 1) {
+    if (free_[0].empty() && free_[1].empty())
+      return fail(BOOST_EAGAIN, "pool has no free block for the copy");
+    refs_[b] -= 1;
+    r.blocks[index] = take(r);
+  }
+  *src = b;
+  *dst = r.blocks[index];
+  return BOOST_OK;
+}
+
+int Dsr::truncate(uint64_t rid, uint32_t n_keep) {
+  auto it = req_.find(rid);
+  if (it == req_.end())
+    return fail(BOOST_EINVAL, "unknown request %llu", (unsigned long long)rid);
+  std::vector<int32_t>& held = it->second.blocks;
+  if (n_keep > held.size())
+    return fail(BOOST_EINVAL, "%u blocks of a request that holds %zu", n_keep, held.size());
+  for (; held.size() > n_keep; held.pop_back()) drop(held.back());
+  return BOOST_OK;
+}
+
+int Dsr::blocks(uint64_t rid, int32_t* out, uint32_t cap, uint32_t* n) const {
+  auto it = req_.find(rid);
+  if (it == req_.end() || !n || (cap && !out))
+    return fail(BOOST_EINVAL, "unknown request %llu", (unsigned long long)rid);
+  const std::vector<int32_t>& held = it->second.blocks;
+  *n = static_cast<uint32_t>(held.size());
+  std::copy_n(held.begin(), std::min<size_t>(cap, held.size()), out);
+  return BOOST_OK;
+}
+
+// The highest held block of a list against the lowest free one, while the
+// free one is lower: afterwards the held blocks of each list are its lowest.
+// A list's blocks have the same host heads, so no request's tier changes.
+int Dsr::compact(uint32_t max_moves, int32_t* src, int32_t* dst, uint32_t* n) {
+  if (!n || (max_moves && (!src || !dst))) return fail(BOOST_EINVAL, "null argument");
+  std::vector<int32_t> to(refs_.size(), -1);  // allocated before anything changes
+  uint32_t moves = 0;
+  for (int t = 0; t < 2; ++t) {
+    std::set<int32_t>& fr = free_[t];
+    for (int32_t b = static_cast<int32_t>(refs_.size()) - 1; b >= 0 && moves < max_moves; --b) {
+      if (refs_[b] == 0 || is_shh_[b] != (t == BOOST_KV_SHH)) continue;
+      if (fr.empty() || *fr.begin() > b) break;
+      auto node = fr.extract(fr.begin());
+      const int32_t d = node.value();
+      node.value() = b;
+      fr.insert(std::move(node));  // the same node: nothing is allocated
+      refs_[d] = refs_[b];
+      refs_[b] = 0;
+      used_hh_ += host_heads_[d];
+      used_hh_ -= host_heads_[b];
+      to[b] = d;
+      src[moves] = b;
+      dst[moves] = d;
+      ++moves;
+    }
+  }
+  for (auto& kv : req_)
+    for (int32_t& b : kv.second.blocks)
+      if (to[b] >= 0) b = to[b];
+  *n = moves;
   return BOOST_OK;
 }
 

@@ -37,6 +37,12 @@ class Dsr {
   int alloc(uint64_t rid, uint32_t n, int32_t* out);
   int release(uint64_t rid);
   int type_of(uint64_t rid, int* type) const;
+  // blocks shared between requests (reference counts)
+  int fork(uint64_t parent, uint64_t child, uint32_t n);
+  int unshare(uint64_t rid, uint32_t index, int32_t* src, int32_t* dst);
+  int truncate(uint64_t rid, uint32_t n_keep);
+  int blocks(uint64_t rid, int32_t* out, uint32_t cap, uint32_t* n) const;
+  int compact(uint32_t max_moves, int32_t* src, int32_t* dst, uint32_t* n);
   uint32_t free_shh() const { return static_cast<uint32_t>(free_[1].size()); }
   uint32_t free_local() const { return static_cast<uint32_t>(free_[0].size()); }
   uint64_t used_blocks() const { return used_; }
@@ -50,8 +56,11 @@ class Dsr {
     int type = 0;
     std::vector<int32_t> blocks;
   };
+  int32_t take(Req& r);  // a free block for r, which may switch lists
+  void drop(int32_t b);  // one holder fewer
   std::set<int32_t> free_[2];  // [BOOST_KV_LOCAL], [BOOST_KV_SHH]
   std::vector<uint8_t> is_shh_, host_heads_;
+  std::vector<uint32_t> refs_;  // requests that hold the block
   std::unordered_map<uint64_t, Req> req_;
   double tau_ = 0.0;
   uint64_t used_ = 0, used_hh_ = 0;

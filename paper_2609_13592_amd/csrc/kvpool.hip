@@ -228,6 +228,69 @@ __global__ __launch_bounds__(256) void kv_read4_kernel(
   v[t * 4 + 3] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
 }
 
+// Blocks copied within the pool: one workgroup per (pair, KV head of K or V,
+// layer), and per (pair, KV head's summary, layer) where the pool has
+// summaries.  Read once and written once: bound by the bytes.
+constexpr int kCopyPairs = 448;  // per launch: the pairs travel as an argument
+struct CopyPairs {
+  int32_t src[kCopyPairs], dst[kCopyPairs];
+};
+struct CopyParams {
+  const char* const* table;  // the pool's pages [layers][2][pages]
+  uint64_t pages;
+  int8_t* index;             // summaries and exponents, or null
+  uint64_t index_blocks;     // layers * H * nb
+  int layer0, H, nb;
+  uint32_t block_bytes;      // bf16: bytes of a head-block
+};
+
+template <bool FP4>
+__global__ __launch_bounds__(256) void copy_blocks_kernel(CopyParams P, CopyPairs pairs) {
+  using namespace bst;
+  const int tid = threadIdx.x;
+  const int s = pairs.src[blockIdx.x], d = pairs.dst[blockIdx.x];
+  const int which = blockIdx.y / P.H, h = blockIdx.y % P.H;
+  const int layer = P.layer0 + static_cast<int>(blockIdx.z);
+  if (which == 2) {
+    const int64_t at = (static_cast<int64_t>(layer) * P.H + h) * P.nb;
+    uint4* const sum = reinterpret_cast<uint4*>(P.index);
+    if (tid < 16) sum[(at + d) * 16 + tid] = sum[(at + s) * 16 + tid];
+    int8_t* const exp = P.index + P.index_blocks * 256;
+    if (tid == 16) exp[at + d] = exp[at + s];
+    return;
+  }
+  const char* const* pt = P.table + (2ull * layer + which) * P.pages;
+  if constexpr (FP4) {
+    const Fp4At a = fp4_at(h, s, P.nb), b = fp4_at(h, d, P.nb);
+    const char* const from = pt[a.page];
+    char* const to = const_cast<char*>(pt[b.page]);
+    const uint32_t off = static_cast<uint32_t>(tid) * 16;
+    if (off < kFp4Code)
+      *reinterpret_cast<uint4*>(to + b.idx * kFp4Code + off) =
+          *reinterpret_cast<const uint4*>(from + a.idx * kFp4Code + off);
+    else if (off < kFp4Code + kFp4Scale)
+      *reinterpret_cast<uint4*>(to + kFp4ScaleAt + b.idx * kFp4Scale + off - kFp4Code) =
+          *reinterpret_cast<const uint4*>(from + kFp4ScaleAt + a.idx * kFp4Scale + off - kFp4Code);
+  } else {
+    const uint64_t a = (static_cast<uint64_t>(h) * P.nb + s) * P.block_bytes;
+    const uint64_t b = (static_cast<uint64_t>(h) * P.nb + d) * P.block_bytes;
+    const uint32_t off = static_cast<uint32_t>(tid) * 16;
+    if (off < P.block_bytes)
+      *reinterpret_cast<uint4*>(const_cast<char*>(pt[b >> 21]) + (b & (kPage - 1)) + off) =
+          *reinterpret_cast<const uint4*>(pt[a >> 21] + (a & (kPage - 1)) + off);
+  }
+}
+
+// The host's exceptions end at the C entry.
+template <typename F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (const std::bad_alloc&) {
+    return bst::fail(BOOST_ENOMEM, "host memory for the allocator state");
+  }
+}
+
 int destroy(boost_kv_pool* p) {
   if (!p) return BOOST_OK;
   if (p->ctx && p->ctx->device >= 0) (void)hipSetDevice(p->ctx->device);
@@ -420,12 +483,39 @@ int boost_kv_block_host_heads(const boost_kv_pool* p, int32_t block, uint32_t* n
 
 int boost_kv_alloc(boost_kv_pool* p, uint64_t rid, uint32_t n, int32_t* out) {
   if (!p) return fail(BOOST_EINVAL, "null pool");
-  return p->dsr.alloc(rid, n, out);
+  return guarded([&] { return p->dsr.alloc(rid, n, out); });
 }
 
 int boost_kv_free(boost_kv_pool* p, uint64_t rid) {
   if (!p) return fail(BOOST_EINVAL, "null pool");
-  return p->dsr.release(rid);
+  return guarded([&] { return p->dsr.release(rid); });
+}
+
+int boost_kv_fork(boost_kv_pool* p, uint64_t parent, uint64_t child, uint32_t n) {
+  if (!p) return fail(BOOST_EINVAL, "null pool");
+  return guarded([&] { return p->dsr.fork(parent, child, n); });
+}
+
+int boost_kv_unshare(boost_kv_pool* p, uint64_t rid, uint32_t index, int32_t* src, int32_t* dst) {
+  if (!p) return fail(BOOST_EINVAL, "null pool");
+  return guarded([&] { return p->dsr.unshare(rid, index, src, dst); });
+}
+
+int boost_kv_truncate(boost_kv_pool* p, uint64_t rid, uint32_t n_keep) {
+  if (!p) return fail(BOOST_EINVAL, "null pool");
+  return guarded([&] { return p->dsr.truncate(rid, n_keep); });
+}
+
+int boost_kv_compact(boost_kv_pool* p, uint32_t max_moves, int32_t* src, int32_t* dst,
+                     uint32_t* n_moves) {
+  if (!p) return fail(BOOST_EINVAL, "null pool");
+  return guarded([&] { return p->dsr.compact(max_moves, src, dst, n_moves); });
+}
+
+int boost_kv_request_blocks(const boost_kv_pool* p, uint64_t rid, int32_t* blocks, uint32_t cap,
+                            uint32_t* n) {
+  if (!p) return fail(BOOST_EINVAL, "null pool");
+  return p->dsr.blocks(rid, blocks, cap, n);
 }
 
 int boost_kv_request_type(const boost_kv_pool* p, uint64_t rid, int* type) {
@@ -492,6 +582,51 @@ int boost_kv_read(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int32
                        static_cast<uint4*>(v), n, H, D, static_cast<int>(p->cfg.block_tokens),
                        static_cast<int>(p->geom.nb));
   BOOST_HIP(hipGetLastError());
+  return BOOST_OK;
+}
+
+int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int n_layers,
+                         const int32_t* src, const int32_t* dst, int n, void* stream) {
+  if (!ctx || !p || !src || !dst) return fail(BOOST_EINVAL, "null argument");
+  if (p->ctx->device < 0 || !p->d_page_table) return fail(BOOST_ENODEV, "plan-only pool");
+  if (layer0 < 0 || n_layers < 1 ||
+      static_cast<int64_t>(layer0) + n_layers > static_cast<int64_t>(p->cfg.layers))
+    return fail(BOOST_EINVAL, "layers [%d, %d + %d) of %u", layer0, layer0, n_layers,
+                p->cfg.layers);
+  if (n < 0) return fail(BOOST_EINVAL, "n=%d", n);
+  const int nb = static_cast<int>(p->geom.nb), H = static_cast<int>(p->cfg.kv_heads);
+  const int tensors = p->d_index ? 3 : 2;
+  if (n_layers > 65535 || static_cast<int64_t>(H) * tensors > 65535)
+    return fail(BOOST_EINVAL, "grid too large");
+  // every destination once, and none of them a source: the order in which
+  // the pairs run then makes no difference
+  const int rc = guarded([&] {
+    std::vector<int32_t> to(dst, dst + n);
+    std::sort(to.begin(), to.end());
+    for (int i = 0; i < n; ++i) {
+      if (src[i] < 0 || src[i] >= nb || dst[i] < 0 || dst[i] >= nb)
+        return fail(BOOST_EINVAL, "pair %d: block %d or %d outside the pool", i, src[i], dst[i]);
+      if (std::binary_search(to.begin(), to.end(), src[i]))
+        return fail(BOOST_EINVAL, "block %d is both read and written", src[i]);
+      if (i && to[i] == to[i - 1]) return fail(BOOST_EINVAL, "block %d is written twice", to[i]);
+    }
+    return BOOST_OK;
+  });
+  if (rc) return rc;
+  const CopyParams P{p->d_page_table, p->geom.pages, p->d_index,
+                     static_cast<uint64_t>(p->cfg.layers) * H * nb, layer0, H, nb,
+                     p->cfg.block_tokens * p->cfg.head_dim * 2};
+  const auto kernel = p->format == BOOST_KV_FP4 ? copy_blocks_kernel<true>
+                                                : copy_blocks_kernel<false>;
+  for (int i = 0; i < n; i += kCopyPairs) {
+    CopyPairs pairs;
+    const int m = std::min(n - i, kCopyPairs);
+    std::copy_n(src + i, m, pairs.src);
+    std::copy_n(dst + i, m, pairs.dst);
+    hipLaunchKernelGGL(kernel, dim3(m, H * tensors, n_layers), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), P, pairs);
+    BOOST_HIP(hipGetLastError());
+  }
   return BOOST_OK;
 }
 
