@@ -163,15 +163,21 @@ def _pairs(case, seed):
 
 
 class State:
-    pool = None
+    pass
+
+
+class _Pool:
+    """The library's pool, given back when neither a state nor a view of its memory needs it any more."""
+
+    def __init__(self, bd, handle):
+        self.bd, self.handle = bd, handle
 
     def __del__(self):
-        if self.pool is not None:
-            try:
-                torch.cuda.synchronize()
-                self.bd.boost_kv_pool_destroy(self.pool)
-            except Exception:  # the interpreter is going down
-                pass
+        try:
+            torch.cuda.synchronize()
+            self.bd.boost_kv_pool_destroy(self.handle)
+        except Exception:  # the interpreter is going down
+            pass
 
 
 _CTX = None
@@ -201,6 +207,7 @@ def _fill(s, case, lens):
             s.ctx, s.bd.KV_FP4 if s.fp4 else s.bd.KV_BF16, 1, case["kv_heads"], HD, max(1, sum(need)),
             case["modulus"] or 2, s.bd.KV_LPP if case["modulus"] else s.bd.KV_ALL_HBM,
             q_heads=case.get("q_heads", case["kv_heads"]), max_batch=len(need), max_blocks_per_seq=s.mb)
+        s.owner = _Pool(s.bd, s.pool)
         take = lambda b, n: s.bd.boost_kv_alloc(s.pool, b, n)  # noqa: E731
     else:
         ids = iter(range(max(1, sum(need))))
@@ -246,7 +253,8 @@ def prepare(case, seed):
             s.bd, s.ctx = _library()
             s.pool = s.bd.boost_kv_pool_create_format(s.ctx, s.bd.KV_BF16, case["layers"], H, HD, 512, 2,
                                                       s.bd.KV_ALL_HBM, max_batch=1, max_blocks_per_seq=1)
-            s.cache = _view(int(s.bd.boost_kv_pages(s.pool, 0, 0)[0]), shape)
+            s.owner = _Pool(s.bd, s.pool)
+            s.cache = _view(int(s.bd.boost_kv_pages(s.pool, 0, 0)[0]), shape, s.owner)
         else:
             s.cache = torch.empty(shape, dtype=torch.bfloat16, device="cuda")
             s.src, s.dst = (torch.from_numpy(v.astype(np.int64)).cuda() for v in (s.src, s.dst))
@@ -291,12 +299,13 @@ def prepare(case, seed):
 
 
 class _Memory:
-    def __init__(self, address, shape):
+    def __init__(self, address, shape, owner):
+        self.owner = owner  # torch keeps this object as long as a tensor of its memory lives
         self.__cuda_array_interface__ = {"data": (address, False), "shape": shape, "typestr": "<i2", "version": 2}
 
 
-def _view(address, shape):
-    return torch.as_tensor(_Memory(address, shape), device="cuda").view(torch.bfloat16)
+def _view(address, shape, owner):
+    return torch.as_tensor(_Memory(address, shape, owner), device="cuda").view(torch.bfloat16)
 
 
 # ---------------------------------------------------------------------------------------- plain forms
