@@ -17,6 +17,11 @@ norms (down's to the next layer's first norm, or the final one), which sum
 them in the order the GEMV's own reduction kernel does: the same bits, one
 launch fewer per projection.
 
+With ``top_blocks`` attention is sparse: after the append the summary of the
+new token's block is brought up to date (index_update), blocks are selected for
+every KV head (select), and attention runs over those (sparse_attn_decode).
+The pool's format (bf16 or 4 bits) makes no difference to the calls.
+
 Weights are [out, in] bf16 matrices placed page by page (each tensor on its
 own, so modulo placement restarts per tensor); norm weights are small bf16
 vectors kept in plain device memory.
@@ -51,12 +56,16 @@ class Dims:
 
 class DecodeModel:
     def __init__(self, ctx: int, dims: Dims, batch: int, max_blocks: int, pool: int,
-                 matrices: dict, norms: dict, fold_slices: bool = True):
+                 matrices: dict, norms: dict, fold_slices: bool = True, top_blocks: int = 0,
+                 first_blocks: int = 1, last_blocks: int = 2):
         """matrices: name -> placed tensor handle for 'embed', 'lm_head' and
         '<kind>.<layer>'; norms: name -> device bf16 tensor for 'norm1.<l>',
         'norm2.<l>', 'norm_f'.  fold_slices: hand the split-K slices of qkv,
         o and down to their consumers (False: every projection reduces its
-        own)."""
+        own).  top_blocks: blocks that each KV head attends to, the context's
+        first_blocks and last_blocks always among them (0: the whole context).
+        The summaries of earlier tokens (a prompt's) are the caller's to bring
+        up to date, with boost_kv_index_update on every layer."""
         import torch
         self.ctx, self.dims, self.B, self.mb, self.pool = ctx, dims, batch, max_blocks, pool
         self.mat, self.norms = matrices, norms
@@ -85,6 +94,11 @@ class DecodeModel:
         self.act = torch.zeros((B, D.ffn), dtype=b16, device=dev)
         self.logits = torch.zeros((B, D.vocab), dtype=f32, device=dev)
         self.ids = torch.zeros((B,), dtype=torch.int32, device=dev)
+        self.top, self.first, self.last = top_blocks, first_blocks, last_blocks
+        if top_blocks:
+            bd.boost_kv_index_enable(pool)
+            self.scores = torch.zeros((B, D.hkv, max_blocks), dtype=f32, device=dev)
+            self.sel = torch.zeros((B, D.hkv, top_blocks), dtype=torch.int32, device=dev)
 
     def step(self, tokens, positions, lens, tables, stream=None, hooks=None):
         """One decode step for the batch.  tokens, positions (= lens - 1),
@@ -123,8 +137,16 @@ class DecodeModel:
                                      F32, s)
                 bd.boost_rope_kv_append(c, self.pool, l, self.qkv, positions, B, D.hq, THETA,
                                         tables, self.mb, self.q, s)
-            bd.boost_paged_attn_decode(c, self.pool, l, self.q, B, D.hq, tables, self.mb,
-                                       lens, 0.0, self.o, BF16, s)
+            if self.top:
+                bd.boost_kv_index_update(c, self.pool, l, tables, self.mb, positions, lens, B, 1,
+                                         s)
+                bd.boost_kv_select(c, self.pool, l, self.q, B, D.hq, tables, self.mb, lens,
+                                   self.top, self.first, self.last, self.scores, self.sel, s)
+                bd.boost_sparse_attn_decode(c, self.pool, l, self.q, B, D.hq, tables, self.mb,
+                                            lens, self.sel, self.top, 0.0, self.o, BF16, s)
+            else:
+                bd.boost_paged_attn_decode(c, self.pool, l, self.q, B, D.hq, tables, self.mb,
+                                           lens, 0.0, self.o, BF16, s)
             if self.fold:
                 S = bd.boost_decode_gemv_slices(c, self.mat[f"o.{l}"], D.d, D.hq * D.hd, self.o,
                                                 B, self.o_sl, bd.MAX_GEMV_SLICES, s)
