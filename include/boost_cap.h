@@ -469,8 +469,7 @@ int boost_kv_pool_create(boost_ctx *ctx, const boost_kv_cfg *cfg,
  * that takes a pool works on both: tokens are handed over and returned as
  * bf16, and attention over a 4-bit pool computes with the values that the
  * codes stand for (q exact, sums and softmax in fp32; probabilities enter the
- * product with V in parts that keep 24 significant bits up to five query
- * heads per KV head, 16 above).  In a 4-bit pool blocks_per_page is 1920, and
+ * product with V with 16 significant bits or more).  In a 4-bit pool blocks_per_page is 1920, and
  * attention takes any q_heads / kv_heads up to 8.
  * Errors: as boost_kv_pool_create; EINVAL (format, head_dim). */
 int boost_kv_pool_create_format(boost_ctx *ctx, const boost_kv_cfg *cfg, int format,

@@ -645,6 +645,90 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   }
 }
 
+// The same sums by W wavefronts, for contexts of many partitions (sparse and
+// 4-bit calls): each takes an equal share of them in order, then the shares
+// are added in order.  The first loads of the sums do not wait for the maxima.
+template <int W>
+__global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
+  __shared__ float s_m[W], s_den[W];
+  __shared__ float2 s_o[W][64];
+  const int bh = blockIdx.x, b = bh / P.Hq;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int L = P.lens[b];
+  const int n_blk = min((L + kT - 1) / kT, P.item_blocks);
+  const int np = L <= 0 ? 0 : (n_blk + P.part_blocks - 1) / P.part_blocks;
+  if (np == 1 && P.one_done) return;  // uniform: the row is written
+  const int per = (np + W - 1) / W, beg = min(np, wave * per), end = min(np, beg + per);
+  const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
+  constexpr int kBatch = 8;
+  float m = -INFINITY, den = 0.f, o0 = 0.f, o1 = 0.f;
+  for (int p0 = beg; p0 < end; p0 += 64) {  // a lane's partition of this round
+    float2 a[kBatch];
+    const int n = min(64, end - p0);
+    auto load = [&](int u0) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        a[u] = *reinterpret_cast<const float2*>(
+            P.part_acc + (base + p0 + min(u0 + u, n - 1)) * kD + lane * 2);
+    };
+    load(0);
+    const float2 ml = lane < n ? *reinterpret_cast<const float2*>(P.part_ml + (base + p0 + lane) * 2)
+                               : make_float2(-INFINITY, 0.f);
+    float M = ml.x;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
+    M = fmaxf(M, m);
+    if (M == -INFINITY) continue;  // uniform: nothing but empty partitions
+    const float c = __builtin_amdgcn_exp2f(m - M);  // m = -inf: 0
+    den *= c;
+    o0 *= c;
+    o1 *= c;
+    m = M;
+    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float wl = w * ml.y;
+    for (int u0 = 0; u0 < n; u0 += kBatch) {
+      if (u0 > 0) load(u0);
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        if (u0 + u >= n) break;  // uniform
+        const float wu = __builtin_bit_cast(
+            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, w), u0 + u));
+        if (wu == 0.f) continue;  // uniform: empty, or of no weight
+        den += __builtin_bit_cast(
+            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wl), u0 + u));
+        o0 = fmaf(a[u].x, wu, o0);
+        o1 = fmaf(a[u].y, wu, o1);
+      }
+    }
+  }
+  s_o[wave][lane] = make_float2(o0, o1);
+  if (lane == 0) {
+    s_m[wave] = m;
+    s_den[wave] = den;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float M = s_m[0];
+#pragma unroll
+  for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w]);
+  den = o0 = o1 = 0.f;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float c = s_m[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w] - M);
+    den = fmaf(s_den[w], c, den);
+    o0 = fmaf(s_o[w][lane].x, c, o0);
+    o1 = fmaf(s_o[w][lane].y, c, o1);
+  }
+  const float inv = den != 0.f ? 1.f / den : 0.f;  // NaN stays one
+  const int64_t oi = static_cast<int64_t>(bh) * kD + lane * 2;
+  if (P.out_bf16) {
+    *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(P.out) + oi) =
+        to_bf16(o0 * inv) | (static_cast<uint32_t>(to_bf16(o1 * inv)) << 16);
+  } else {
+    *reinterpret_cast<float2*>(static_cast<float*>(P.out) + oi) = make_float2(o0 * inv, o1 * inv);
+  }
+}
+
 template <int G, bool SEL>
 int launch_partitions(AttnParams& P, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
@@ -668,8 +752,14 @@ int launch(AttnParams& P, hipStream_t s) {
   return P.sel ? launch_partitions<G, true>(P, s) : launch_partitions<G, false>(P, s);
 }
 
-int launch_merge(AttnParams& P, hipStream_t s) {
-  hipLaunchKernelGGL(attn_merge, dim3(static_cast<unsigned>(P.B * P.Hq)), dim3(64), 0, s, P);
+int launch_merge(AttnParams& P, bool wide, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(P.B * P.Hq));
+  if (wide && P.n_parts > 32)
+    hipLaunchKernelGGL(attn_merge_wide<16>, grid, dim3(1024), 0, s, P);
+  else if (wide)
+    hipLaunchKernelGGL(attn_merge_wide<4>, grid, dim3(256), 0, s, P);
+  else
+    hipLaunchKernelGGL(attn_merge, grid, dim3(64), 0, s, P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }
@@ -737,7 +827,9 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   // enough work items to fill the GPU several times over (so the last grid
   // wave is short), each long enough to amortise its start and its merge
   // (PART_MIN blocks) and short enough to balance (PART_MAX blocks)
-  const int want_parts = std::max(1, (BOOST_ATTN_ITEMS + B * H - 1) / (B * H));
+  const bool fp4 = pool->format == BOOST_KV_FP4;
+  const int items = fp4 ? BOOST_ATTN_ITEMS4 : BOOST_ATTN_ITEMS;
+  const int want_parts = std::max(1, (items + B * H - 1) / (B * H));
   int part_min = kPartMin;
   while (part_min > kPartFew &&
          static_cast<int64_t>(B) * H * ((max_blocks + part_min - 1) / part_min) < ctx->n_cu)
@@ -746,6 +838,8 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
       {kMaxPartBlocks, max_blocks,
        std::max(part_min, std::min(kPartMax, (max_blocks + want_parts - 1) / want_parts))});
   P.part_blocks = std::max(P.part_blocks, 4);
+  // a 4-bit context of one partition needs no merge
+  if (fp4 && max_blocks <= kOneBlocks) P.part_blocks = std::max(max_blocks, 4);
   P.n_parts = (max_blocks + P.part_blocks - 1) / P.part_blocks;
   P.max_parts = max_parts > 0 ? max_parts : P.n_parts;
   if (P.n_parts > P.max_parts) return fail(BOOST_EINVAL, "partition scratch too small");
@@ -756,13 +850,15 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   P.scale = scale > 0.f ? scale : 1.0f / std::sqrt(static_cast<float>(kD));
   P.part_acc = part_acc;
   P.part_ml = part_ml;
+  P.one_done = fp4;
   P.out = out;
   P.out_bf16 = out_dtype == BOOST_DTYPE_BF16;
   auto s = static_cast<hipStream_t>(stream);
   int rc;
-  if (pool->format == BOOST_KV_FP4) {
+  if (fp4) {
     if (G > 8) return fail(BOOST_EINVAL, "Hq/H=%d above 8", G);
     rc = launch_fp4(P, s);
+    if (P.n_parts == 1) return rc;
   } else {
     switch (G) {
       case 1: rc = launch<1>(P, s); break;
@@ -772,7 +868,7 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
       default: return fail(BOOST_EINVAL, "Hq/H=%d not in {1, 2, 4, 8}", G);
     }
   }
-  return rc ? rc : launch_merge(P, s);
+  return rc ? rc : launch_merge(P, sel || fp4, s);
 }
 
 }  // namespace

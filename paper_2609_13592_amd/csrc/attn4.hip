@@ -1,29 +1,36 @@
 // a5 over a 4-bit pool: GQA paged-attention decode whose K and V are E2M1
 // codes with a power-of-two scale per token and 32 dims (kvfmt.h).
 //
-// Work items, partitions and the merge are those of the bf16 kernel
-// (attn_items.h).  Within an item every wavefront takes pairs of blocks (32
-// tokens) in turn, on the matrix cores:
+// Work items and partitions are those of the bf16 kernel (attn_items.h); a
+// context of one partition is finished by its workgroup, the others leave
+// partial sums for the merge.  Within an item every wavefront takes pairs of
+// blocks (32 tokens) in turn, on the matrix cores:
 //
-//   scores  S[t, c] = sum_d K[t, d] q[c, d], one 16x16x32 product per group of
-//           8 dims of each quad: lane (r, qd) holds token r's codes of group
-//           qd, one 16-byte load, converted to bf16 with the group's scale
-//           (exact: a code has two significant bits, the scale is a power of
-//           two).  q is bf16, so every product is exact and the sum is fp32.
+//   scores  S[t, c] = sum_d K[t, d] q[c, d], one 16x16x32 product per 8 dims
+//           of each group: lane (r, qd) holds token r's codes of group qd, one
+//           16-byte load, converted to bf16 with the group's scale (exact: a
+//           code has two significant bits, the scale is a power of two).  q is
+//           bf16, so every product is exact and the sum is fp32.
 //   softmax the result leaves tokens 4 qd .. 4 qd + 3 of column c in a lane;
 //           running maximum and sum per column in fp32.
-//   output  O[d, c] += sum_t V[t, d] p[t, c]: the probabilities stay in the
+//   output  O[d, c] = sum_t V[t, d] p[t, c]: the probabilities stay in the
 //           lanes that computed them, because the sum over t may run in any
 //           order as long as V's operand follows it: lane (r, qd) holds tokens
-//           4 qd .. 4 qd + 3 of dims 16 i + r (i = 0..7), again one 16-byte load.
+//           4 qd .. 4 qd + 3 of dims 8 r .. 8 r + 7, again one 16-byte load.
+//           A conversion gives two neighbouring dims of one token, where an
+//           operand register wants two terms of the sum: they are taken as two
+//           terms, and a column's register holds (p, 0) or (0, p), so that it
+//           sums the even dims alone or the odd ones.  No value is moved.
 //
-// Columns: a call has G = Hq / H query heads to 16 columns, so head j also
-// stands in columns G + j and 2 G + j, and each copy multiplies V by another
-// part of the fp32 probability (its first 8 significant bits, the next 8, the
-// rest; with G > 5 there are two copies and the second holds the rest rounded
-// to 8 bits).  The parts' outputs are added in fp32 at the end: the precision
-// of fp32 probabilities (G > 5: 16 to 17 bits) at no further matrix work.
+// Columns: a call has G = Hq / H query heads to 16 columns.  Up to four heads,
+// column c is head c % 4, odd or even dims by bit 2, and by bit 3 one of two
+// parts of the fp32 probability: its first 8 significant bits, or the rest
+// rounded to 8.  Up to eight heads, bit 3 is odd or even, and the parts are two
+// products into the same sums.  Either way p enters with 16 to 17 bits, an
+// error of 2^-17 of each p at most, below what fp32 scores of 128 products
+// carry.
 #include <cmath>
+#include <type_traits>
 
 #include "attn_items.h"
 #include "kvfmt.h"
@@ -37,103 +44,113 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int kCols = 16;
-constexpr int kAccRow = kD + 4;  // floats of a column's row in LDS (banks)
+constexpr float kLowest = 3.402823466e+38f;
+constexpr int kAccRow = kD + 4;  // floats of a head's row in LDS (banks)
 
 __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Maximum (or sum) of v over the four lanes that hold one column.
-__device__ __forceinline__ float col_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-__device__ __forceinline__ float col_sum(float v) {
-  v += __shfl_xor(v, 16, 64);
-  return v + __shfl_xor(v, 32, 64);
+// v of the four lanes that hold one column (16 and 32 lanes apart) by F, the
+// same bits in each of them.
+template <typename F>
+__device__ __forceinline__ float over_column(float v, F f) {
+  const uint32_t u = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t w = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
 
 // One block's codes and scales in a lane.
 struct Block4 {
-  u32x4 k, v;   // 32 codes of token r, group qd; four tokens of dims 16 i + r
-  u32x4 vs;     // scale bytes of tokens 4 qd .. 4 qd + 3, a byte per group
+  u32x4 k, v;   // 32 codes of token r, group qd; four tokens of dims 8 r ..
   uint32_t ks;  // scale byte of token r, group qd
-  int tok;      // tokens that count (0: none, nothing was read)
+  uint32_t vs;  // scale bytes of tokens 4 qd .., group r / 4
+  int tok;      // tokens that count
 };
 
-template <int PARTS, bool WAVE, bool SEL>
+// EIGHT: more than four query heads per KV head.  ONE: no context has more
+// than one partition: a workgroup for every (KV head, request), empty ones too.
+enum class Items { kWave, kGroup, kOne };
+template <bool EIGHT, Items ITEMS, bool SEL>
 __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
-  __shared__ float s_acc[4][kCols][kAccRow];
-  __shared__ float s_ml[4][kCols][2];
+  __shared__ float s_acc[4][8][kAccRow];  // heads (EIGHT), else 4 heads of each part
+  __shared__ float s_ml[4][8][2];
   __shared__ int32_t row[kMaxPartBlocks];    // the partition's pool blocks
   __shared__ int32_t s_tok[kMaxPartBlocks];  // and their tokens that count
   __shared__ int s_red[4], s_pick[5];
   int part, b, g, L;
-  if constexpr (WAVE) {
+  if constexpr (ITEMS == Items::kWave) {
     if (!item_of_wave(P, blockIdx.x, b, g, part, L)) return;  // uniform
-  } else {
+  } else if constexpr (ITEMS == Items::kGroup) {
     if (!item_of(P, blockIdx.x, b, g, part, L, s_red, row, s_pick)) return;  // uniform
+    __syncthreads();  // row has served the search
+  } else {
+    b = blockIdx.x % P.B;
+    g = P.H - 1 - blockIdx.x / P.B;
+    part = 0;
+    L = P.lens[b];
   }
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r = lane & 15, qd = lane >> 4;
   const int G = P.Hq / P.H;
-  const int n_blk = L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks);
+  const int n_blk = L <= 0 ? 0 : min((L - 1) / kT + 1, P.item_blocks);
   const int blk_beg = part * P.part_blocks;
-  if (blk_beg >= n_blk) return;  // uniform
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
-  __syncthreads();  // row has served the item search
-  if (tid < nbp) {
+  const bool whole = n_blk <= P.part_blocks;
+  for (int i = tid; i < nbp; i += kThreads) {
     int tok;
     int32_t blk;
     if constexpr (SEL) {
-      blk = selected(P, b, g, blk_beg + tid, L, tok);
+      blk = selected(P, b, g, blk_beg + i, L, tok);
     } else {
-      blk = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk_beg + tid];
-      tok = min(kT, L - (blk_beg + tid) * kT);
+      blk = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk_beg + i];
+      tok = min(kT, L - (blk_beg + i) * kT);
     }
     // a block outside the pool counts as if it were not in the context
     const bool ok = blk >= 0 && blk < P.nb;
-    row[tid] = ok ? blk : 0;
-    s_tok[tid] = ok ? tok : 0;
+    row[i] = ok ? blk : 0;
+    s_tok[i] = ok ? tok : 0;
   }
-  // queries: column r is head r % G, dims 32 qd + 8 s .. + 7 in operand s
+  constexpr int kHeads = EIGHT ? 8 : 4;
+  const int head = r % kHeads;  // this column's, if below G
+  const bool odd = r & kHeads;  // odd dims
+  const bool rest = !EIGHT && (r & 8);  // the second part of p
+  // queries: dims 32 qd + 8 s .. + 7 in operand s
   u32x4 bq[4];
   {
-    const int j = r % G;
     const uint4* q = reinterpret_cast<const uint4*>(
-        P.q + (static_cast<int64_t>(b) * P.Hq + g * G + j) * kD + 32 * qd);
+        P.q + (static_cast<int64_t>(b) * P.Hq + g * G + min(head, G - 1)) * kD + 32 * qd);
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const uint4 u = q[s];
       bq[s] = u32x4{u.x, u.y, u.z, u.w};
     }
   }
-  const int copy = r / G;  // which part of the probabilities this column takes
+  const uint32_t code_off = lane * 16, ks_off = lane, vs_off = bst::fp4_v_scale_at(4 * qd, r / 4);
   __syncthreads();
 
   const uint32_t first_host = static_cast<uint32_t>(P.host_from >> 21);
+  // Block i of the partition; past its end the last one with no token that
+  // counts, so that loads need no branch (a block outside the pool: block 0).
   auto fetch = [&](int i, Block4& x) {
-    x.k = x.v = x.vs = u32x4{0, 0, 0, 0};
-    x.ks = 0;
-    x.tok = 0;
-    if (i >= nbp) return;  // uniform over the wavefront
-    x.tok = __builtin_amdgcn_readfirstlane(s_tok[i]);
-    if (x.tok == 0) return;
-    const bst::Fp4At at = bst::fp4_at(g, __builtin_amdgcn_readfirstlane(row[i]), P.nb);
+    const int at_i = min(i, nbp - 1);
+    const int tok = __builtin_amdgcn_readfirstlane(s_tok[at_i]);
+    x.tok = i < nbp ? tok : 0;
+    const bst::Fp4At at = bst::fp4_at(g, __builtin_amdgcn_readfirstlane(row[at_i]), P.nb);
     const bool host = at.page >= first_host;
     const uint64_t off = static_cast<uint64_t>(host ? at.page - first_host : at.page) << 21;
     const char* const pk = (host ? P.k_host : P.k_hbm) + off;
     const char* const pv = (host ? P.v_host : P.v_hbm) + off;
     const uint32_t code = at.idx * bst::kFp4Code, sc = bst::kFp4ScaleAt + at.idx * bst::kFp4Scale;
-    x.k = *reinterpret_cast<const u32x4*>(pk + code + r * 64 + qd * 16);
-    x.ks = *reinterpret_cast<const uint8_t*>(pk + sc + r * 4 + qd);
-    x.v = *reinterpret_cast<const u32x4*>(pv + code + lane * 16);
-    x.vs = *reinterpret_cast<const u32x4*>(pv + sc + qd * 16);
+    x.k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pk + code + code_off));
+    x.ks = *reinterpret_cast<const uint8_t*>(pk + sc + ks_off);
+    x.v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pv + code + code_off));
+    x.vs = *reinterpret_cast<const uint32_t*>(pv + sc + vs_off);
   };
   const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
-  // a block's scores in the log2 domain: -inf for tokens that do not count
   auto scores = [&](const Block4& x) {
     const float ks = bst::fp4_scale(x.ks);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -143,97 +160,125 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
                        fp4_unpack<2>(x.k[i], ks), fp4_unpack<3>(x.k[i], ks)};
       s = mfma(a, bq[i], s);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = 4 * qd + i < x.tok ? s[i] * sc2 : -INFINITY;
     return s;
   };
-  // V^T of the 16-dim tiles 2 g, 2 g + 1: four tokens of the lane's dim,
-  // packed in pairs (a token that does not count is left out by a finite
-  // scale, since its probability 0 must not meet a NaN)
-  auto values = [&](const Block4& x, uint32_t (*t)[2]) {
-    u32x4 vs = x.vs;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) vs[i] = 4 * qd + i < x.tok ? vs[i] : 0;
-    auto tile = [&](auto sel, int gr) {
-      constexpr int SELB = decltype(sel)::value;
-      uint32_t c[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // the scale byte moved to the exponent; the bits around it do not count
-        const uint32_t e = SELB == 0 ? vs[i] << 23 : SELB == 1 ? vs[i] << 15
-                           : SELB == 2 ? vs[i] << 7 : vs[i] >> 1;
-        c[i] = fp4_unpack<SELB>(x.v[i], __uint_as_float(e));
-      }
-      t[2 * gr][0] = __builtin_amdgcn_perm(c[1], c[0], 0x05040100);
-      t[2 * gr][1] = __builtin_amdgcn_perm(c[3], c[2], 0x05040100);
-      t[2 * gr + 1][0] = __builtin_amdgcn_perm(c[1], c[0], 0x07060302);
-      t[2 * gr + 1][1] = __builtin_amdgcn_perm(c[3], c[2], 0x07060302);
-    };
-    tile(std::integral_constant<int, 0>{}, 0);
-    tile(std::integral_constant<int, 1>{}, 1);
-    tile(std::integral_constant<int, 2>{}, 2);
-    tile(std::integral_constant<int, 3>{}, 3);
+  // dims 8 r + 2 B, + 1 of the lane's four tokens; the scale byte is moved to
+  // the exponent, the bits around it do not count
+  auto values = [&](const Block4& x, auto byte) {
+    constexpr int B = decltype(byte)::value;
+    return u32x4{fp4_unpack<B>(x.v[0], __uint_as_float(x.vs << 23)),
+                 fp4_unpack<B>(x.v[1], __uint_as_float(x.vs << 15)),
+                 fp4_unpack<B>(x.v[2], __uint_as_float(x.vs << 7)),
+                 fp4_unpack<B>(x.v[3], __uint_as_float(x.vs >> 1))};
   };
-  // this column's part of a probability
-  auto share = [&](float p) {
-    const float p0 = __uint_as_float(__float_as_uint(p) & 0xffff0000u);
-    if constexpr (PARTS == 2) return copy == 0 ? p0 : p - p0;
-    const float p1 = p - p0, p10 = __uint_as_float(__float_as_uint(p1) & 0xffff0000u);
-    return copy == 0 ? p0 : copy == 1 ? p10 : p1 - p10;
+  // A probability's part for this column: its first 16 bits, in the lower or
+  // the upper half of the register by place, or the rest of them.
+  const uint32_t place = odd ? 0x07060c0cu : 0x0c0c0706u;  // 0x0c: a zero byte
+  auto first = [&](float p) { return __builtin_amdgcn_perm(__float_as_uint(p), 0u, place); };
+  auto second = [&](float p) {
+    const float x = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+    return __builtin_amdgcn_perm(__float_as_uint(x) + 0x8000u, 0u, place);
   };
-  auto pack = [&](float lo, float hi) {
-    typedef __attribute__((ext_vector_type(2))) float f32x2;
-    return __builtin_bit_cast(uint32_t,
-                              __builtin_convertvector(f32x2{lo, hi}, bst::bf16x2));
+  // without a branch over the columns: the mask is all ones in the columns of
+  // the second part
+  const uint32_t off = rest ? 0xffff0000u : 0u, round = rest ? 0x8000u : 0u;
+  auto either = [&](float p) {
+    const float x = p - __uint_as_float(__float_as_uint(p) & off);
+    return __builtin_amdgcn_perm(__float_as_uint(x) + round, 0u, place);
   };
 
-  float m = -INFINITY, l = 0.f;
-  f32x4 acc[8];
+  // m starts at the lowest finite value: exp2(-inf - m) is 0 from the first
+  // token on, also while none has counted
+  float m = -kLowest, l = 0.f;
+  f32x4 acc[4];  // dims 8 (4 qd + i) + 2 byte + odd
 #pragma unroll
-  for (int i = 0; i < 8; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int i = 2 * wave; i < nbp; i += 8) {
-    Block4 x0, x1;
-    fetch(i, x0);
-    fetch(i + 1, x1);
-    const f32x4 s0 = scores(x0), s1 = scores(x1);
-    float mc = m;
+  for (int i = 0; i < 4; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto consume = [&](Block4& x0, Block4& x1) {
+    f32x4 s0 = scores(x0), s1 = scores(x1);
+    if (x0.tok + x1.tok < 2 * kT) {  // uniform: some tokens do not count
 #pragma unroll
-    for (int e = 0; e < 4; ++e) mc = fmaxf(mc, fmaxf(s0[e], s1[e]));
-    mc = col_max(mc);
+      for (int e = 0; e < 4; ++e) {
+        const bool in0 = 4 * qd + e < x0.tok, in1 = 4 * qd + e < x1.tok;
+        s0[e] = in0 ? s0[e] : -INFINITY;
+        s1[e] = in1 ? s1[e] : -INFINITY;
+        // their probability 0 must not meet a NaN: a finite scale
+        x0.vs &= in0 ? ~0u : ~(255u << (8 * e));
+        x1.vs &= in1 ? ~0u : ~(255u << (8 * e));
+      }
+    }
+    float mc = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
+                     fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
+    mc = fmaxf(m, over_column(mc, [](float a, float b) { return fmaxf(a, b); }) * sc2);
     if (__any(mc > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mc);
+      const float c = __builtin_amdgcn_exp2f(m - mc);
       l *= c;
 #pragma unroll
-      for (int t = 0; t < 8; ++t) acc[t] *= c;
+      for (int t = 0; t < 4; ++t) acc[t] *= c;
       m = mc;
     }
     float p[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      // -inf: a token that does not count (also where the maximum still is -inf)
-      p[e] = s0[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s0[e] - m);
-      p[4 + e] = s1[e] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s1[e] - m);
+      p[e] = __builtin_amdgcn_exp2f(fmaf(s0[e], sc2, -m));
+      p[4 + e] = __builtin_amdgcn_exp2f(fmaf(s1[e], sc2, -m));
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) l += p[e];
-    u32x4 bp;
+    u32x4 b0, b1, c0, c1;  // the parts of p (EIGHT: the second in c)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) bp[e] = pack(share(p[2 * e]), share(p[2 * e + 1]));
-    uint32_t t0[8][2], t1[8][2];
-    values(x0, t0);
-    values(x1, t1);
-#pragma unroll
-    for (int t = 0; t < 8; ++t)
-      acc[t] = mfma(u32x4{t0[t][0], t0[t][1], t1[t][0], t1[t][1]}, bp, acc[t]);
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (EIGHT) {
+        b0[e] = first(p[e]);
+        b1[e] = first(p[4 + e]);
+        c0[e] = second(p[e]);
+        c1[e] = second(p[4 + e]);
+      } else {
+        b0[e] = either(p[e]);
+        b1[e] = either(p[4 + e]);
+      }
+    }
+    auto tile = [&](auto byte) {
+      constexpr int B = decltype(byte)::value;
+      const u32x4 v0 = values(x0, byte), v1 = values(x1, byte);
+      acc[B] = mfma(v0, b0, acc[B]);
+      acc[B] = mfma(v1, b1, acc[B]);
+      if constexpr (EIGHT) {
+        acc[B] = mfma(v0, c0, acc[B]);
+        acc[B] = mfma(v1, c1, acc[B]);
+      }
+    };
+    tile(std::integral_constant<int, 0>{});
+    tile(std::integral_constant<int, 1>{});
+    tile(std::integral_constant<int, 2>{});
+    tile(std::integral_constant<int, 3>{});
+  };
+  if (nbp > 0) {
+    // The next pair's loads are out while a pair is computed.  They are issued
+    // without a branch (past the end: the last block again, from the caches),
+    // so that the waits can count them.
+    Block4 a0, a1, b0, b1;
+    fetch(2 * wave, a0);
+    fetch(2 * wave + 1, a1);
+    for (int i = 2 * wave; i < nbp; i += 16) {
+      fetch(i + 8, b0);
+      fetch(i + 9, b1);
+      consume(a0, a1);
+      if (i + 8 >= nbp) break;  // uniform over the wavefront
+      fetch(i + 16, a0);
+      fetch(i + 17, a1);
+      consume(b0, b1);
+    }
   }
-  l = col_sum(l);
-  if (r < PARTS * G) {
+  l = over_column(l, [](float a, float b) { return a + b; });
+  {
+    float* const to = &s_acc[wave][EIGHT ? head : head + (rest ? 4 : 0)][32 * qd + (odd ? 1 : 0)];
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
-      *reinterpret_cast<f32x4*>(&s_acc[wave][r][16 * t + 4 * qd]) = acc[t];
-    if (qd == 0) {
-      s_ml[wave][r][0] = m;
-      s_ml[wave][r][1] = l;
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < 4; ++t) to[8 * i + 2 * t] = acc[t][i];
+    if (lane < kHeads) {
+      s_ml[wave][lane][0] = m;
+      s_ml[wave][lane][1] = l;
     }
   }
   __syncthreads();
@@ -241,36 +286,59 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
   // from the largest, at the common maximum
   for (int e = tid; e < G * (kD / 4); e += kThreads) {
     const int j = e / (kD / 4), d4 = e % (kD / 4) * 4;
-    float M = -INFINITY, sum = 0.f;
+    float M = -kLowest, sum = 0.f;
 #pragma unroll
     for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ml[w][j][0]);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float mw = s_ml[w][j][0];
-      const float c = mw == M ? 1.f : __builtin_amdgcn_exp2f(mw - M);
+      const float c = __builtin_amdgcn_exp2f(s_ml[w][j][0] - M);
       sum += s_ml[w][j][1] * c;
-      f32x4 a = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int u = 0; u < PARTS; ++u)
-        a += *reinterpret_cast<const f32x4*>(&s_acc[w][u * G + j][d4]);
+      f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][j][d4]);
+      if constexpr (!EIGHT) a += *reinterpret_cast<const f32x4*>(&s_acc[w][j + 4][d4]);
       o += a * c;
     }
-    const int64_t at = (static_cast<int64_t>(b) * P.Hq + g * G + j) * P.max_parts + part;
+    const int64_t out = static_cast<int64_t>(b) * P.Hq + g * G + j;
+    if (whole) {  // uniform
+      const float inv = sum != 0.f ? 1.f / sum : 0.f;  // nothing counted: a zero row
+      o *= inv;
+      if (P.out_bf16) {
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(P.out) + out * kD + d4) =
+            make_uint2(to_bf16(o[0]) | static_cast<uint32_t>(to_bf16(o[1])) << 16,
+                       to_bf16(o[2]) | static_cast<uint32_t>(to_bf16(o[3])) << 16);
+      } else {
+        float* const to = static_cast<float*>(P.out) + out * kD + d4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = o[i];
+      }
+      continue;
+    }
+    const int64_t at = out * P.max_parts + part;
     *reinterpret_cast<f32x4*>(P.part_acc + at * kD + d4) = o;
     if (d4 == 0) {
-      P.part_ml[at * 2] = sum == sum ? M : 0.f;  // NaN must not look empty to the merge
+      // nothing counted: what the merge takes for empty (a NaN is not)
+      P.part_ml[at * 2] = sum == 0.f ? -INFINITY : M;
       P.part_ml[at * 2 + 1] = sum;
     }
   }
 }
 
-template <int PARTS, bool SEL>
+template <bool EIGHT, Items ITEMS>
 void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
-  if (P.B <= 64)
-    hipLaunchKernelGGL((attn4_partition<PARTS, true, SEL>), dim3(grid), dim3(kThreads), 0, s, P);
+  if (P.sel)
+    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, true>), dim3(grid), dim3(kThreads), 0, s, P);
   else
-    hipLaunchKernelGGL((attn4_partition<PARTS, false, SEL>), dim3(grid), dim3(kThreads), 0, s, P);
+    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, false>), dim3(grid), dim3(kThreads), 0, s, P);
+}
+
+template <bool EIGHT>
+void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
+  if (P.n_parts == 1)
+    launch<EIGHT, Items::kOne>(P, grid, s);
+  else if (P.B <= 64)
+    launch<EIGHT, Items::kWave>(P, grid, s);
+  else
+    launch<EIGHT, Items::kGroup>(P, grid, s);
 }
 
 }  // namespace
@@ -281,11 +349,10 @@ namespace attn {
 int launch_fp4(AttnParams& P, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
   if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "grid too large");
-  const unsigned n = static_cast<unsigned>(grid);
-  if (P.Hq / P.H <= 5)
-    P.sel ? launch<3, true>(P, n, s) : launch<3, false>(P, n, s);
+  if (P.Hq / P.H <= 4)
+    launch<false>(P, static_cast<unsigned>(grid), s);
   else
-    P.sel ? launch<2, true>(P, n, s) : launch<2, false>(P, n, s);
+    launch<true>(P, static_cast<unsigned>(grid), s);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

@@ -15,6 +15,19 @@ constexpr int kT = 16;           // tokens per block
 #ifndef BOOST_ATTN_ITEMS
 #define BOOST_ATTN_ITEMS 2048
 #endif
+// A 4-bit item carries a quarter of the bytes, so fewer are aimed for (64
+// requests of 512..4096: 36.5 us with 768, 37.5 with 1024, two of 100000 44.0
+// and 45.5; with 2048 5 to 10 % more)
+#ifndef BOOST_ATTN_ITEMS4
+#define BOOST_ATTN_ITEMS4 768
+#endif
+// 4-bit contexts of up to this many blocks stay whole: a launch without a
+// merge (one request of 301 tokens 4.9 us, cut in five 7.2; of 800 tokens 7.4
+// either way, of 1000 8.1 and 7.4; 64 requests of 1000 15.7 and 21.9)
+#ifndef BST_ONE
+#define BST_ONE 50
+#endif
+constexpr int kOneBlocks = BST_ONE;
 constexpr int kMaxPartBlocks = 256;         // blocks per partition, at most
 static_assert(kMaxPartBlocks <= kThreads, "one thread per partition size");
 // A work item of fewer than 16 blocks spends as long on its start (q loads)
@@ -61,6 +74,7 @@ struct AttnParams {
   float* part_ml;   // [B * Hq * max_parts][2] running max, sum of p
   void* out;
   int out_bf16;
+  int one_done;  // contexts of one partition are finished without the merge
 };
 
 __device__ __forceinline__ uint16_t to_bf16(float f) {
@@ -288,6 +302,8 @@ __device__ __forceinline__ int32_t selected(const AttnParams& P, int b, int g, i
 }
 
 // The kernels of a 4-bit pool: launches the partitions (any Hq / H up to 8).
+// Contexts of one partition are finished there; if none has more (n_parts 1),
+// empty ones too, and there is nothing to merge.
 int launch_fp4(AttnParams& P, hipStream_t s);
 
 }  // namespace attn

@@ -299,27 +299,25 @@ __device__ __forceinline__ void store_row4(char* page, uint32_t idx, int tok, bo
   const uint32_t sa = fp4_scale_byte(am << 16), sb = fp4_scale_byte(bm << 16);
   const float fa = __uint_as_float(static_cast<uint32_t>(a) << 16);
   const float fb = __uint_as_float(static_cast<uint32_t>(b) << 16);
-  // the other value of this lane's byte: the odd dim of a pair (K), dim + 16 (V)
-  const int far = is_v ? 16 : 1;
-  const float oa = __shfl_xor(fa, far, 64), ob = __shfl_xor(fb, far, 64);
+  // the odd dim of the pair in this lane's byte
+  const float oa = __shfl_xor(fa, 1, 64), ob = __shfl_xor(fb, 1, 64);
   const uint32_t ca = fp4_pack<0>(0u, fa, oa, fp4_scale(sa));
   const uint32_t cb = fp4_pack<0>(0u, fb, ob, fp4_scale(sb));
   char* const code = page + idx * kFp4Code;
   const int g = i >> 5;  // groups g and g + 2
-  if (!(i & far)) {
+  if (!(i & 1)) {
     if (is_v) {
-      char* const dw = code + (tok / 4) * 256 + (i & 15) * 16 + (tok % 4) * 4;
-      dw[g] = static_cast<char>(ca);
-      dw[g + 2] = static_cast<char>(cb);
+      code[fp4_v_code_at(tok, i / 8) + i % 8 / 2] = static_cast<char>(ca);
+      code[fp4_v_code_at(tok, 8 + i / 8) + i % 8 / 2] = static_cast<char>(cb);
     } else {
-      code[tok * 64 + i / 2] = static_cast<char>(ca);
-      code[tok * 64 + 32 + i / 2] = static_cast<char>(cb);
+      code[fp4_k_code_at(tok, g) + i % 32 / 2] = static_cast<char>(ca);
+      code[fp4_k_code_at(tok, g + 2) + i % 32 / 2] = static_cast<char>(cb);
     }
   }
   if (!(i & 31)) {
-    char* const sc = page + kFp4ScaleAt + idx * kFp4Scale + tok * 4;
-    sc[g] = static_cast<char>(sa);
-    sc[g + 2] = static_cast<char>(sb);
+    char* const sc = page + kFp4ScaleAt + idx * kFp4Scale;
+    sc[is_v ? fp4_v_scale_at(tok, g) : fp4_k_scale_at(tok, g)] = static_cast<char>(sa);
+    sc[is_v ? fp4_v_scale_at(tok, g + 2) : fp4_k_scale_at(tok, g + 2)] = static_cast<char>(sb);
   }
 }
 

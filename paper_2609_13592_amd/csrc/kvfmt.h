@@ -13,16 +13,17 @@
 // holds kFp4Page head-blocks: their 1024 code bytes first, then their 64
 // scale bytes, so a page's tier is the tier of all that belongs to its blocks.
 //
-//   K codes  [token][dim / 2], the even dim in the low nibble: the 16 bytes at
-//            token * 64 + 16 * g are group g of the token, which is what one
-//            lane of a matrix-core operand holds (row = token).
-//   V codes  [token / 4][r][token % 4][g], r = dim % 16: byte g of a token's
-//            dword r holds dims 32 g + r (low nibble) and 32 g + 16 + r, so
+//   K codes  [group][token][16 bytes], the even dim in the low nibble: what one
+//            lane of a matrix-core operand holds (row = token), the lanes of a
+//            wavefront one after another (64 bytes apart, a head-block took
+//            twice the cache accesses).
+//   V codes  [token / 4][r][token % 4]: the dword of dims 8 r .. 8 r + 7, so
 //            the 16 bytes at 256 * (token / 4) + 16 * r are what one lane
-//            holds of the transposed operand (row = dim, four tokens of every
-//            16-dim tile), and a token's bytes are its own: two tokens are
+//            holds of the transposed operand: four tokens of eight dims that
+//            share a scale.  A token's bytes are its own: two tokens are
 //            written at once without a race.
-//   scales   [token][4], K and V alike.
+//   scales   K [group][token]; V [token / 4][group][token % 4], the four of
+//            such a lane in one dword.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -62,6 +63,17 @@ __device__ __forceinline__ uint32_t fp4_scale_byte(uint32_t amax_bits) {
 // byte 0 (exponent field 0) is 2^-127 and 255 gives NaN.
 __device__ __forceinline__ float fp4_scale(uint32_t byte) {
   return __uint_as_float(byte << 23);
+}
+
+// Byte offset of a token's scale of group g among a head-block's 64.
+__device__ __forceinline__ uint32_t fp4_k_scale_at(int tok, int g) { return g * 16 + tok; }
+__device__ __forceinline__ uint32_t fp4_v_scale_at(int tok, int g) {
+  return (tok / 4) * 16 + g * 4 + tok % 4;
+}
+// ... of its K codes of group g, and of its V codes' dword r.
+__device__ __forceinline__ uint32_t fp4_k_code_at(int tok, int g) { return g * 256 + tok * 16; }
+__device__ __forceinline__ uint32_t fp4_v_code_at(int tok, int r) {
+  return (tok / 4) * 256 + r * 16 + (tok % 4) * 4;
 }
 
 // Codes of a (low nibble) and b (high nibble): round to nearest, ties to the

@@ -14,6 +14,7 @@
 // machine.  257 bytes stand for the 8 KiB (bf16) of a head-block.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "kvfmt.h"
 #include "runtime.h"
@@ -26,6 +27,7 @@ constexpr int kSum = 2 * kD;      // bytes of a summary: hi, then lo
 constexpr int kNotFinite = 127;   // exponent byte of a block with an inf or NaN key
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 struct IndexParams {
   const char* const* pt_k;  // this layer's K pages
@@ -48,15 +50,66 @@ __device__ __forceinline__ float pow2f(int e) {  // -126 <= e <= 127
 }
 __device__ __forceinline__ float lo_bf16(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1)
-    v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), m, 64)));
-  return v;
+
+// Two bf16 values as two 16-bit integers in the same order (its own inverse;
+// NaNs lie beyond the infinities of their sign), so that two extremes take one
+// instruction each.
+typedef __attribute__((ext_vector_type(2))) short i16x2;
+__device__ __forceinline__ i16x2 ordered(uint32_t v) {
+  const i16x2 x = __builtin_bit_cast(i16x2, v);
+  return x ^ ((x >> 15) & static_cast<short>(0x7fff));
+}
+__device__ __forceinline__ uint32_t values_of(i16x2 x) {
+  return __builtin_bit_cast(uint32_t, x ^ ((x >> 15) & static_cast<short>(0x7fff)));
+}
+__device__ __forceinline__ i16x2 max2(i16x2 a, i16x2 b) { return __builtin_elementwise_max(a, b); }
+__device__ __forceinline__ i16x2 min2(i16x2 a, i16x2 b) { return __builtin_elementwise_min(a, b); }
+constexpr short kNone = -32768;  // below every value (and, negated less one, above)
+
+// The value of another lane of the 16-lane row: CTRL is a DPP pattern.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return static_cast<uint32_t>(
+      __builtin_amdgcn_mov_dpp(static_cast<int>(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kXor1 = 0xb1, kXor2 = 0x4e, kXor7 = 0x141, kXor8 = 0x128;
+template <int CTRL>
+__device__ __forceinline__ i16x2 dpp2(i16x2 v) {
+  return __builtin_bit_cast(i16x2, dpp<CTRL>(__builtin_bit_cast(uint32_t, v)));
+}
+// The largest v of the row's 16 lanes, in each of them.
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+  v = max(v, dpp<kXor1>(v));
+  v = max(v, dpp<kXor2>(v));
+  v = max(v, dpp<kXor7>(v));
+  return max(v, dpp<kXor8>(v));
+}
+// v of the lanes 16 and 32 apart by f.
+template <typename F>
+__device__ __forceinline__ uint32_t over_rows(uint32_t v, F f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(b[0], b[1]);
+}
+
+// The larger magnitude, as bf16 bits, of extremes hi (largest) and lo
+// (smallest) in both halves.
+__device__ __forceinline__ uint32_t magnitude(i16x2 hi, i16x2 lo) {
+  const uint32_t h = values_of(hi), l = values_of(lo);
+  // the magnitude of the largest value counts if it is not negative, that of
+  // the smallest if it is
+  auto one = [](uint32_t hv, uint32_t lv) {
+    const uint32_t a = hv & 0x8000u ? 0u : hv, b = lv & 0x8000u ? lv & 0x7fffu : 0u;
+    return max(a, b);
+  };
+  return max(one(h & 0xffffu, l & 0xffffu), one(h >> 16, l >> 16));
 }
 
 // One wavefront per head-block.  FP4: lane (token r, group qd); else lane
-// (8-dim chunk, token row qd of four).
+// (8-dim chunk r, token row qd of four).  Bound by the keys' bytes: the
+// extremes of two dims take one instruction, and no lane's value goes through
+// LDS.
 template <bool FP4>
 __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int chunks) {
   const int lane = threadIdx.x & 63, r = lane & 15, qd = lane >> 4;
@@ -69,105 +122,113 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int ch
   const int last = (end - 1) / kT;
   for (int blk = start / kT + chunk * 4 + static_cast<int>(threadIdx.x >> 6); blk <= last;
        blk += chunks * 4) {
-    const int32_t id = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk];
+    const int32_t id = __builtin_amdgcn_readfirstlane(
+        P.tables[static_cast<int64_t>(b) * P.max_blocks + blk]);
     if (id < 0 || id >= P.nb) continue;  // uniform over the wavefront
     const int live = min(kT, end - blk * kT);
     const int64_t at = static_cast<int64_t>(g) * P.nb + id;
     int8_t* const out = P.sum + at * kSum;
-    uint32_t amax = 0;  // bf16 bits
     if constexpr (FP4) {
       using namespace bst;
       const Fp4At f = fp4_at(g, id, P.nb);
       const char* const page = P.pt_k[f.page];
-      const uint4 c = *reinterpret_cast<const uint4*>(page + f.idx * kFp4Code + r * 64 + qd * 16);
-      const uint32_t sb = static_cast<uint8_t>(
-          page[kFp4ScaleAt + f.idx * kFp4Scale + r * 4 + qd]);
+      const uint4 c = *reinterpret_cast<const uint4*>(page + f.idx * kFp4Code + lane * 16);
+      const float s = fp4_scale(
+          static_cast<uint8_t>(page[kFp4ScaleAt + f.idx * kFp4Scale + lane]));
       const bool in = r < live;
-      const float s = fp4_scale(sb);
-      float mx[32], mn[32];
       const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+      i16x2 mx[16], mn[16];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t p[4] = {fp4_unpack<0>(w[i], s), fp4_unpack<1>(w[i], s),
+        const uint32_t v[4] = {fp4_unpack<0>(w[i], s), fp4_unpack<1>(w[i], s),
                                fp4_unpack<2>(w[i], s), fp4_unpack<3>(w[i], s)};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          amax = max(amax, max(p[j] & 0x7fffu, (p[j] >> 16) & 0x7fffu));
-          mx[8 * i + 2 * j] = in ? lo_bf16(p[j]) : -INFINITY;
-          mx[8 * i + 2 * j + 1] = in ? hi_bf16(p[j]) : -INFINITY;
-          mn[8 * i + 2 * j] = in ? lo_bf16(p[j]) : INFINITY;
-          mn[8 * i + 2 * j + 1] = in ? hi_bf16(p[j]) : INFINITY;
+          const i16x2 x = ordered(v[j]);
+          mx[4 * i + j] = in ? x : i16x2{kNone, kNone};
+          mn[4 * i + j] = in ? x : i16x2{-1 - kNone, -1 - kNone};
         }
       }
-      amax = wave_max(in ? amax : 0);
       // over the 16 tokens, half of the dims kept in each step: lane r ends
       // with dims 2 r, 2 r + 1 of its group
+      auto step = [&](auto ctrl, auto count, bool up) {
+        constexpr int C = decltype(ctrl)::value, N = decltype(count)::value;
 #pragma unroll
-      for (int n = 16, m = 8; m >= 1; n >>= 1, m >>= 1) {
-        const bool up = lane & m;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (i >= n) break;
-          const float keep_x = up ? mx[n + i] : mx[i], give_x = up ? mx[i] : mx[n + i];
-          const float keep_n = up ? mn[n + i] : mn[i], give_n = up ? mn[i] : mn[n + i];
-          mx[i] = fmaxf(keep_x, __shfl_xor(give_x, m, 64));
-          mn[i] = fminf(keep_n, __shfl_xor(give_n, m, 64));
+        for (int i = 0; i < N; ++i) {
+          const i16x2 kx = up ? mx[N + i] : mx[i], gx = up ? mx[i] : mx[N + i];
+          const i16x2 kn = up ? mn[N + i] : mn[i], gn = up ? mn[i] : mn[N + i];
+          mx[i] = max2(kx, dpp2<C>(gx));
+          mn[i] = min2(kn, dpp2<C>(gn));
         }
-      }
-      const int e = amax >= 0x7f80 ? kNotFinite : step_exponent(amax);
-      const float step = pow2f(e == kNotFinite ? 0 : -e);
+      };
+      using std::integral_constant;
+      // (lanes xor 8, 7, 2, 1: together all 16 of a row)
+      step(integral_constant<int, kXor8>{}, integral_constant<int, 8>{}, lane & 8);
+      step(integral_constant<int, kXor7>{}, integral_constant<int, 4>{}, lane & 4);
+      step(integral_constant<int, kXor2>{}, integral_constant<int, 2>{}, lane & 2);
+      step(integral_constant<int, kXor1>{}, integral_constant<int, 1>{}, lane & 1);
+      uint32_t amax = row_max(magnitude(mx[0], mn[0]));
+      amax = over_rows(amax, [](uint32_t a, uint32_t b) { return max(a, b); });
+      const bool bad = amax >= 0x7f80;  // no numbers to keep
+      const int e = bad ? kNotFinite : step_exponent(amax);
+      const float scale = pow2f(bad ? 0 : -e);
+      const uint32_t hx = values_of(mx[0]), hn = values_of(mn[0]);
+      const char2 hi = {static_cast<signed char>(ceilf(lo_bf16(hx) * scale)),
+                        static_cast<signed char>(ceilf(hi_bf16(hx) * scale))};
+      const char2 lo = {static_cast<signed char>(floorf(lo_bf16(hn) * scale)),
+                        static_cast<signed char>(floorf(hi_bf16(hn) * scale))};
       int8_t* const o = out + 32 * qd + 2 * r;
-      const bool bad = e == kNotFinite;  // no numbers to keep
-      *reinterpret_cast<char2*>(o) =
-          bad ? char2{0, 0}
-              : char2{static_cast<signed char>(ceilf(mx[0] * step)),
-                      static_cast<signed char>(ceilf(mx[1] * step))};
-      *reinterpret_cast<char2*>(o + kD) =
-          bad ? char2{0, 0}
-              : char2{static_cast<signed char>(floorf(mn[0] * step)),
-                      static_cast<signed char>(floorf(mn[1] * step))};
+      *reinterpret_cast<char2*>(o) = bad ? char2{0, 0} : hi;
+      *reinterpret_cast<char2*>(o + kD) = bad ? char2{0, 0} : lo;
       if (lane == 0) P.exp[at] = static_cast<int8_t>(e);
     } else {
       const uint64_t byte = static_cast<uint64_t>(at) * kT * kD * 2;
-      const char* const src = P.pt_k[byte >> 21] + (byte & (bst::kPage - 1)) + r * 16;
-      float mx[8], mn[8];
+      const char* const src = P.pt_k[byte >> 21] + (byte & (bst::kPage - 1)) + lane * 16;
+      u32x4 u[4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        mx[i] = -INFINITY;
-        mn[i] = INFINITY;
+      for (int i = 0; i < 4; ++i)  // token 4 i + qd
+        u[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + i * 1024));
+      i16x2 mx[4], mn[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        mx[j] = i16x2{kNone, kNone};
+        mn[j] = i16x2{-1 - kNone, -1 - kNone};
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int t = 4 * i + qd;
-        const uint4 u = *reinterpret_cast<const uint4*>(src + t * kD * 2);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-        if (t < live) {
+        const bool in = 4 * i + qd < live;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            amax = max(amax, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-            mx[2 * j] = fmaxf(mx[2 * j], lo_bf16(w[j]));
-            mx[2 * j + 1] = fmaxf(mx[2 * j + 1], hi_bf16(w[j]));
-            mn[2 * j] = fminf(mn[2 * j], lo_bf16(w[j]));
-            mn[2 * j + 1] = fminf(mn[2 * j + 1], hi_bf16(w[j]));
-          }
+        for (int j = 0; j < 4; ++j) {
+          const i16x2 x = ordered(u[i][j]);
+          mx[j] = max2(mx[j], in ? x : i16x2{kNone, kNone});
+          mn[j] = min2(mn[j], in ? x : i16x2{-1 - kNone, -1 - kNone});
         }
       }
-      amax = wave_max(amax);
+      uint32_t amax = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], 16, 64));
-        mx[i] = fmaxf(mx[i], __shfl_xor(mx[i], 32, 64));
-        mn[i] = fminf(mn[i], __shfl_xor(mn[i], 16, 64));
-        mn[i] = fminf(mn[i], __shfl_xor(mn[i], 32, 64));
+      for (int j = 0; j < 4; ++j) {
+        mx[j] = __builtin_bit_cast(i16x2, over_rows(__builtin_bit_cast(uint32_t, mx[j]), [](uint32_t a, uint32_t b) {
+          return __builtin_bit_cast(uint32_t, max2(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+        }));
+        mn[j] = __builtin_bit_cast(i16x2, over_rows(__builtin_bit_cast(uint32_t, mn[j]), [](uint32_t a, uint32_t b) {
+          return __builtin_bit_cast(uint32_t, min2(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+        }));
+        amax = max(amax, magnitude(mx[j], mn[j]));
       }
-      const int e = amax >= 0x7f80 ? kNotFinite : step_exponent(amax);
-      const float step = pow2f(e == kNotFinite ? 0 : -e);
+      amax = row_max(amax);
+      const bool bad = amax >= 0x7f80;
+      const int e = bad ? kNotFinite : step_exponent(amax);
+      const float scale = pow2f(bad ? 0 : -e);
       uint32_t w[2] = {0, 0};
-      if (e != kNotFinite) {
+      if (!bad) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int v = static_cast<int>(qd == 0 ? ceilf(mx[i] * step) : floorf(mn[i] * step));
-          w[i / 4] |= (static_cast<uint32_t>(v) & 255u) << (8 * (i % 4));
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t v = values_of(qd == 0 ? mx[j] : mn[j]);
+          const float x = lo_bf16(v) * scale, y = hi_bf16(v) * scale;
+          const int p = static_cast<int>(qd == 0 ? ceilf(x) : floorf(x));
+          const int q = static_cast<int>(qd == 0 ? ceilf(y) : floorf(y));
+          w[j / 2] |= ((static_cast<uint32_t>(p) & 255u) | (static_cast<uint32_t>(q) & 255u) << 8)
+                      << (16 * (j % 2));
         }
       }
       if (qd < 2) *reinterpret_cast<uint2*>(out + qd * kD + r * 8) = make_uint2(w[0], w[1]);
@@ -193,20 +254,43 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
   return L <= 0 ? 0 : min((L - 1) / kT + 1, P.max_blocks);
 }
 
-// Scores of 16-block tiles, one wavefront a tile: rows are blocks, columns
-// the KV head's query heads, the 256 products of a pair in four 16x16x64
-// integer products (hi against the positive part of q8, lo against the
-// negative).  Bound by the summaries' bytes.
-constexpr int kTileBlocks = 16, kTilesPerWave = 4;
-constexpr int kScoreBlocks = 4 * kTileBlocks * kTilesPerWave;  // per workgroup
+// Scores of 16-block tiles, four to a wavefront: rows are blocks, columns the
+// KV head's query heads, the 256 products of a pair in four 16x16x64 integer
+// products (hi against the positive part of q8, lo against the negative).
+// Bound by the summaries' bytes; the loads of all four tiles are out together,
+// and q is rounded while they are.
+constexpr int kTileBlocks = 16, kTiles = 4;
+constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
 __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int chunks) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
   const int chunk = blockIdx.x % chunks, bg = blockIdx.x / chunks;
   const int g = bg % P.H, b = bg / P.H;
   const int n = context_blocks(P, b);
-  if (chunk * kScoreBlocks >= n) return;  // uniform
+  const int first = chunk * kScoreBlocks + wave * kTiles * kTileBlocks;
+  if (first >= n) return;  // uniform over the wavefront; no barrier follows
   const int G = P.Hq / P.H;
+  const int8_t* const sum = P.sum + static_cast<int64_t>(g) * P.nb * kSum;
+  const int8_t* const exps = P.exp + static_cast<int64_t>(g) * P.nb;
+  const int32_t* const table = P.tables + static_cast<int64_t>(b) * P.max_blocks;
+  int32_t id[kTiles];
+  i32x4 a[kTiles][4];
+  int e[kTiles];  // of block (row) r; -128: no such block
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const int blk = first + i * kTileBlocks + r;
+    id[i] = table[min(blk, n - 1)];
+  }
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    const bool ok = id[i] >= 0 && id[i] < P.nb;
+    id[i] = ok ? id[i] : 0;
+    const i32x4* s = reinterpret_cast<const i32x4*>(sum + static_cast<int64_t>(id[i]) * kSum) + qd;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) a[i][j] = s[4 * j];
+    e[i] = exps[id[i]];
+    e[i] = ok ? e[i] : -128;
+  }
   // column r: head r (zero beyond G), dims 16 qd .. + 15 and 64 more
   i32x4 qb[4];
   int eq;
@@ -224,11 +308,10 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) amax = max(amax, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-    amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), 16, 64)));
-    amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), 32, 64)));
+    amax = over_rows(amax, [](uint32_t x, uint32_t y) { return max(x, y); });
     const bool none = amax >= 0x7f80 || r >= G;  // a query that is not finite counts as 0
     eq = none ? 0 : step_exponent(amax);
-    const float step = pow2f(-eq);
+    const float step = none ? 0.f : pow2f(-eq);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t pos[2], neg[2];
@@ -239,6 +322,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
         for (int j = 0; j < 4; ++j) {
           const uint32_t x = w[4 * i + 2 * h + j / 2];
           const float f = (j & 1 ? hi_bf16(x) : lo_bf16(x)) * step;
+          // (a NaN or infinity times 0 is a NaN: fminf and fmaxf drop it)
           const int v = none ? 0 : static_cast<int>(fminf(fmaxf(rintf(f), -127.f), 127.f));
           pos[h] |= (static_cast<uint32_t>(max(v, 0)) & 255u) << (8 * j);
           neg[h] |= (static_cast<uint32_t>(min(v, 0)) & 255u) << (8 * j);
@@ -250,124 +334,182 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
       qb[2 + i / 2][2 * (i % 2) + 1] = static_cast<int>(neg[1]);
     }
   }
-  const int8_t* const sum = P.sum + static_cast<int64_t>(g) * P.nb * kSum;
-  const int8_t* const exps = P.exp + static_cast<int64_t>(g) * P.nb;
-  const int32_t* const table = P.tables + static_cast<int64_t>(b) * P.max_blocks;
   float* const to = P.scores + (static_cast<int64_t>(b) * P.H + g) * P.max_blocks;
-#pragma unroll 1
-  for (int i = 0; i < kTilesPerWave; ++i) {
-    const int first = chunk * kScoreBlocks + (i * 4 + wave) * kTileBlocks;
-    if (first >= n) break;  // uniform over the wavefront
-    const int blk = first + r;
-    int32_t id = blk < n ? table[blk] : -1;
-    const bool ok = id >= 0 && id < P.nb;
-    id = ok ? id : 0;
-    i32x4 a[4] = {};
-    if (ok) {
-      const i32x4* s = reinterpret_cast<const i32x4*>(sum + static_cast<int64_t>(id) * kSum) + qd;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) a[j] = s[4 * j];
-    }
-    const int e = ok ? exps[id] : -128;  // -128: no such block
+  for (int i = 0; i < kTiles; ++i) {
+    const int row0 = first + i * kTileBlocks;
+    if (row0 >= n) break;  // uniform over the wavefront
     i32x4 c = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[j], qb[j], c, 0, 0, 0);
-    // lane (column r, rows 4 qd ..): the row's exponent, the largest column
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i][j], qb[j], c, 0, 0, 0);
+    // the exponents of rows 4 qd .. 4 qd + 3: those of a quad of lanes in one
+    // word, then the word of quad qd
+    uint32_t quad = static_cast<uint32_t>(e[i]) & 255u;
+    const uint32_t pair = dpp<kXor1>(quad);
+    quad = r & 1 ? quad << 8 | pair : quad | pair << 8;
+    const uint32_t other = dpp<kXor2>(quad);
+    quad = r & 2 ? quad << 16 | other : quad | other << 16;
+    const uint32_t q0 = __builtin_amdgcn_readlane(quad, 0), q1 = __builtin_amdgcn_readlane(quad, 4);
+    const uint32_t q2 = __builtin_amdgcn_readlane(quad, 8), q3 = __builtin_amdgcn_readlane(quad, 12);
+    const uint32_t er4 = qd == 0 ? q0 : qd == 1 ? q1 : qd == 2 ? q2 : q3;
     float v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int er = __shfl(e, 4 * qd + j, 64);
+      const int er = static_cast<int8_t>(er4 >> (8 * j));
+      // the largest column (of up to 16 heads)
       float x = r < G ? ldexpf(static_cast<float>(c[j]), er + eq) : -INFINITY;
-#pragma unroll
-      for (int m = 8; m >= 1; m >>= 1) x = fmaxf(x, __shfl_xor(x, m, 64));
+      auto larger = [](float p, uint32_t q) { return fmaxf(p, __uint_as_float(q)); };
+      x = larger(x, dpp<kXor1>(__float_as_uint(x)));
+      x = larger(x, dpp<kXor2>(__float_as_uint(x)));
+      x = larger(x, dpp<kXor7>(__float_as_uint(x)));
+      x = larger(x, dpp<kXor8>(__float_as_uint(x)));
       v[j] = er == -128 ? -INFINITY : er == kNotFinite ? INFINITY : x;
     }
-    if (r < 4 && first + 4 * qd + r < n)
-      to[first + 4 * qd + r] = r == 0 ? v[0] : r == 1 ? v[1] : r == 2 ? v[2] : v[3];
+    if (r < 4 && row0 + 4 * qd + r < n)
+      to[row0 + 4 * qd + r] = r == 0 ? v[0] : r == 1 ? v[1] : r == 2 ? v[2] : v[3];
   }
 }
 
-// The order of a score as an unsigned key; blocks that are always taken
-// stand above every score.
-__device__ __forceinline__ uint32_t key_of(const SelectParams& P, const float* scores, int i,
-                                           int n) {
-  if (i < P.n_first || i >= n - P.n_last) return 0xffffffffu;
-  const uint32_t u = __float_as_uint(scores[i] + 0.f);  // -0 as 0: they are equal
-  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
-}
-
 // One workgroup per (request, KV head): the top_k-th largest key by its
-// digits (256 bins, four passes), then the blocks above it and the first of
-// those equal to it, in order.
-constexpr int kSelThreads = 256;
-__global__ __launch_bounds__(kSelThreads) void select_blocks_kernel(SelectParams P) {
-  __shared__ int hist[256], s_wave[2][kSelThreads / 64], s_pick[2];
+// digits, then the keys above it and the first of those equal to it, in order.
+// A thread owns consecutive blocks, V of them in registers (what lies past
+// V * NT blocks is read again in every pass), so that the ranks of all take
+// one scan.  The digits start at the highest bit in which any two keys differ
+// (scores of one query differ little in their exponents; from bit 31 on, most
+// keys would meet in one counter), and end when no key is left to decide.
+template <int NT, int V>
+__global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
+  constexpr int kWaves = NT / 64;
+  __shared__ int hist[256], s_a[kWaves], s_b[kWaves], s_pick[3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / P.H;
   const int n = context_blocks(P, b);
   int32_t* const sel = P.sel + static_cast<int64_t>(blockIdx.x) * P.top_k;
   if (n <= P.top_k) {  // uniform: every block
-    for (int i = tid; i < P.top_k; i += kSelThreads) sel[i] = i < n ? i : -1;
+    for (int i = tid; i < P.top_k; i += NT) sel[i] = i < n ? i : -1;
     return;
   }
   const float* const scores = P.scores + static_cast<int64_t>(blockIdx.x) * P.max_blocks;
-  uint32_t prefix = 0;
-  int need = P.top_k;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelThreads) {
-      const uint32_t k = key_of(P, scores, i, n);
-      if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&hist[(k >> shift) & 255], 1);
-    }
-    __syncthreads();
-    // keys with a digit of at least 255 - tid
-    const int own = hist[255 - tid];
-    int x = own;
+  // blocks that are always taken stand above every score
+  auto key_at = [&](int i) {
+    if (i < P.n_first || i >= n - P.n_last) return 0xffffffffu;
+    const uint32_t u = __float_as_uint(scores[i] + 0.f);  // -0 as 0: they are equal
+    return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+  };
+  const int per = (n + NT - 1) / NT, beg = min(n, tid * per), cnt = min(n, beg + per) - beg;
+  uint32_t key[V];
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int y = __shfl_up(x, d, 64);
-      if (lane >= d) x += y;
-    }
-    if (lane == 63) s_wave[0][wave] = x;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) x += s_wave[0][w];
-    if (x >= need && x - own < need) {
-      s_pick[0] = 255 - tid;
-      s_pick[1] = need - (x - own);
-    }
-    __syncthreads();
-    prefix |= static_cast<uint32_t>(s_pick[0]) << shift;
-    need = s_pick[1];
-    __syncthreads();
+  for (int j = 0; j < V; ++j) key[j] = j < cnt ? key_at(beg + j) : 0;
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j < cnt) f(key[j], beg + j);
+    for (int j = V; j < cnt; ++j) f(key_at(beg + j), beg + j);
+  };
+  // bits in which keys differ: those that are set somewhere and clear somewhere
+  uint32_t any1 = 0, any0 = 0;
+  each([&](uint32_t k, int) {
+    any1 |= k;
+    any0 |= ~k;
+  });
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    any1 |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(any1), m, 64));
+    any0 |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(any0), m, 64));
   }
-  // need: how many of the keys equal to prefix are taken, lowest index first
-  int above = 0, equal = 0;  // before this chunk
-  for (int base = 0; base < n; base += kSelThreads) {
-    const int i = base + tid;
-    const uint32_t k = i < n ? key_of(P, scores, i, n) : 0;
-    const bool gt = i < n && k > prefix, eq = i < n && k == prefix;
-    const unsigned long long mg = __ballot(gt), me = __ballot(eq);
-    if (lane == 0) {
-      s_wave[0][wave] = __popcll(mg);
-      s_wave[1][wave] = __popcll(me);
-    }
+  if (lane == 0) {
+    s_a[wave] = static_cast<int>(any1);
+    s_b[wave] = static_cast<int>(any0);
+  }
+  __syncthreads();
+  any1 = any0 = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    any1 |= static_cast<uint32_t>(s_a[w]);
+    any0 |= static_cast<uint32_t>(s_b[w]);
+  }
+  const uint32_t differ = any1 & any0;
+  // (all equal: the keys at and above any1 & ~any0, none above)
+  uint32_t least = any1 & ~any0;  // the bits that all share; then the decided ones
+  int need = P.top_k;             // of the keys whose decided bits equal least's
+  int top = differ ? 32 - __clz(static_cast<int>(differ)) : 0;  // undecided bits
+  least = top == 32 ? 0 : least >> top << top;
+  bool open = true;
+  while (open && top > 0) {
+    const int shift = max(0, top - 8);
+    const uint32_t digit = (1u << (top - shift)) - 1;
+    for (int i = tid; i < 256; i += NT) hist[i] = 0;
     __syncthreads();
-    int g0 = above, e0 = equal;
-    for (int w = 0; w < kSelThreads / 64; ++w) {
-      if (w < wave) {
-        g0 += s_wave[0][w];
-        e0 += s_wave[1][w];
+    each([&](uint32_t k, int) {
+      if (top == 32 || (k ^ least) >> top == 0) atomicAdd(&hist[(k >> shift) & digit], 1);
+    });
+    __syncthreads();
+    // the first wavefront: keys with a digit of at least 255 - 4 lane - j
+    if (wave == 0) {
+      int c[4], x = 0;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        c[j] = hist[255 - 4 * lane - j];
+        x += c[j];
       }
-      above += s_wave[0][w];
-      equal += s_wave[1][w];
+      int before = x;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int y = __shfl_up(before, d, 64);
+        if (lane >= d) before += y;
+      }
+      before -= x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (before < need && before + c[j] >= need) {
+          s_pick[0] = 255 - 4 * lane - j;
+          s_pick[1] = need - before;
+          s_pick[2] = c[j];
+        }
+        before += c[j];
+      }
     }
-    const unsigned long long below = (1ull << lane) - 1;
-    g0 += __popcll(mg & below);
-    e0 += __popcll(me & below);
-    if (gt || (eq && e0 < need)) sel[g0 + min(e0, need)] = i;
     __syncthreads();
+    least |= static_cast<uint32_t>(s_pick[0]) << shift;
+    need = s_pick[1];
+    open = s_pick[2] != need;  // else all keys of this digit are taken
+    top = shift;
   }
+  // keys above least's decided bits are taken, and the first `need` of those
+  // that equal them
+  int above = 0, equal = 0;
+  auto place = [&](uint32_t k) { return top == 32 ? 0 : (k >> top) == (least >> top) ? 0 : k > least ? 1 : -1; };
+  each([&](uint32_t k, int) {
+    const int c = place(k);
+    above += c > 0;
+    equal += c == 0;
+  });
+  __syncthreads();  // s_a and s_b are free again
+  int x = above, y = equal;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int u = __shfl_up(x, d, 64), v = __shfl_up(y, d, 64);
+    if (lane >= d) {
+      x += u;
+      y += v;
+    }
+  }
+  if (lane == 63) {
+    s_a[wave] = x;
+    s_b[wave] = y;
+  }
+  __syncthreads();
+  x -= above;
+  y -= equal;
+  for (int w = 0; w < wave; ++w) {
+    x += s_a[w];
+    y += s_b[w];
+  }
+  each([&](uint32_t k, int i) {
+    const int c = place(k);
+    if (c > 0 || (c == 0 && y < need)) sel[x + min(y, need)] = i;
+    x += c > 0;
+    y += c == 0;
+  });
 }
 
 }  // namespace
@@ -455,8 +597,12 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   hipLaunchKernelGGL(block_scores_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, P,
                      chunks);
   BOOST_HIP(hipGetLastError());
-  hipLaunchKernelGGL(select_blocks_kernel, dim3(static_cast<unsigned>(B) * H), dim3(kSelThreads),
-                     0, s, P);
+  // a workgroup as wide as the widest context has work for
+  const dim3 rows(static_cast<unsigned>(B) * H);
+  if (max_blocks <= 2048)
+    hipLaunchKernelGGL((select_blocks_kernel<256, 8>), rows, dim3(256), 0, s, P);
+  else
+    hipLaunchKernelGGL((select_blocks_kernel<1024, 8>), rows, dim3(1024), 0, s, P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

@@ -56,42 +56,8 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
   v[t] = *reinterpret_cast<const uint4*>(pt_v[page] + in);
 }
 
-// ---- 4 bits: one lane per (token, head, group of 32 dims), the four groups
-// of a token in the four lanes of a quad.  Bound by the bytes: 256 in and 68
-// out per row (or the reverse).
-
-template <int K>
-__device__ __forceinline__ uint32_t quad_lane(uint32_t v) {
-  return static_cast<uint32_t>(
-      __builtin_amdgcn_mov_dpp(static_cast<int>(v), K * 0x55, 0xf, 0xf, true));
-}
-
-// Lane c of a quad gets in x[b] lane b's w[c] (a transpose of dwords over the
-// quad).
-__device__ __forceinline__ void quad_transpose(const uint32_t* w, int c, uint32_t* x) {
-  uint32_t a[4][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    a[i][0] = quad_lane<0>(w[i]);
-    a[i][1] = quad_lane<1>(w[i]);
-    a[i][2] = quad_lane<2>(w[i]);
-    a[i][3] = quad_lane<3>(w[i]);
-  }
-#pragma unroll
-  for (int b = 0; b < 4; ++b) x[b] = c == 0 ? a[0][b] : c == 1 ? a[1][b] : c == 2 ? a[2][b] : a[3][b];
-}
-
-// Byte j of y[i] is byte i of x[j].
-__device__ __forceinline__ void byte_transpose(const uint32_t* x, uint32_t* y) {
-  const uint32_t a0 = __builtin_amdgcn_perm(x[1], x[0], 0x05010400);  // bytes 0, 1 of x0, x1
-  const uint32_t a1 = __builtin_amdgcn_perm(x[3], x[2], 0x05010400);
-  const uint32_t b0 = __builtin_amdgcn_perm(x[1], x[0], 0x07030602);  // bytes 2, 3
-  const uint32_t b1 = __builtin_amdgcn_perm(x[3], x[2], 0x07030602);
-  y[0] = __builtin_amdgcn_perm(a1, a0, 0x05040100);
-  y[1] = __builtin_amdgcn_perm(a1, a0, 0x07060302);
-  y[2] = __builtin_amdgcn_perm(b1, b0, 0x05040100);
-  y[3] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
-}
+// ---- 4 bits: one lane per (token, head, group of 32 dims).  Bound by the
+// bytes: 256 in and 68 out per row (or the reverse).
 
 // 32 bf16 values (64 bytes at src) as floats, and their scale byte.
 __device__ __forceinline__ uint32_t load_group(const uint4* src, float* f) {
@@ -132,12 +98,31 @@ __device__ __forceinline__ int64_t slot_of(const RowSlot& r, int64_t i, int nb) 
   return slot < static_cast<int64_t>(nb) * bst::kFp4Tok ? slot : -1;
 }
 
+// The codes of 32 values, eight to a dword.
+__device__ __forceinline__ void group_codes(const float* f, float s, uint32_t* w) {
+  using namespace bst;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = fp4_pack<0>(0u, f[8 * i], f[8 * i + 1], s);
+    w[i] = fp4_pack<1>(w[i], f[8 * i + 2], f[8 * i + 3], s);
+    w[i] = fp4_pack<2>(w[i], f[8 * i + 4], f[8 * i + 5], s);
+    w[i] = fp4_pack<3>(w[i], f[8 * i + 6], f[8 * i + 7], s);
+  }
+}
+
+// Eight bf16 values of a dword of codes.
+__device__ __forceinline__ uint4 code_values(uint32_t c, float s) {
+  using namespace bst;
+  return make_uint4(fp4_unpack<0>(c, s), fp4_unpack<1>(c, s), fp4_unpack<2>(c, s),
+                    fp4_unpack<3>(c, s));
+}
+
 __global__ __launch_bounds__(256) void kv_write4_kernel(
     const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v, RowSlot rows,
     const uint4* __restrict__ k, const uint4* __restrict__ v, int n, int H, int nb) {
   using namespace bst;
   const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (t >= static_cast<int64_t>(n) * H * 4) return;  // whole quads
+  if (t >= static_cast<int64_t>(n) * H * 4) return;
   const int g = static_cast<int>(t & 3);
   const int64_t th = t >> 2;
   const int h = static_cast<int>(th % H);
@@ -147,37 +132,19 @@ __global__ __launch_bounds__(256) void kv_write4_kernel(
   const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
   char* const pk = const_cast<char*>(pt_k[at.page]);
   char* const pv = const_cast<char*>(pt_v[at.page]);
-  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale + tok * 4 + g;
+  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale;
   float f[32];
-  uint32_t sb = load_group(k + t * 4, f);
-  float s = fp4_scale(sb);
-  uint32_t w[4], x[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {  // dims 8 i .. 8 i + 7 of the group
-    w[i] = fp4_pack<0>(0u, f[8 * i], f[8 * i + 1], s);
-    w[i] = fp4_pack<1>(w[i], f[8 * i + 2], f[8 * i + 3], s);
-    w[i] = fp4_pack<2>(w[i], f[8 * i + 4], f[8 * i + 5], s);
-    w[i] = fp4_pack<3>(w[i], f[8 * i + 6], f[8 * i + 7], s);
-  }
-  *reinterpret_cast<uint4*>(pk + code + tok * 64 + g * 16) = make_uint4(w[0], w[1], w[2], w[3]);
-  pk[scale] = static_cast<char>(sb);
+  uint32_t sb = load_group(k + t * 4, f), w[4];
+  group_codes(f, fp4_scale(sb), w);
+  *reinterpret_cast<uint4*>(pk + code + fp4_k_code_at(tok, g)) =
+      make_uint4(w[0], w[1], w[2], w[3]);
+  pk[scale + fp4_k_scale_at(tok, g)] = static_cast<char>(sb);
   sb = load_group(v + t * 4, f);
-  s = fp4_scale(sb);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {  // bytes r = 4 i .. 4 i + 3: dims r and 16 + r of the group
-    w[i] = fp4_pack<0>(0u, f[4 * i], f[16 + 4 * i], s);
-    w[i] = fp4_pack<1>(w[i], f[4 * i + 1], f[16 + 4 * i + 1], s);
-    w[i] = fp4_pack<2>(w[i], f[4 * i + 2], f[16 + 4 * i + 2], s);
-    w[i] = fp4_pack<3>(w[i], f[4 * i + 3], f[16 + 4 * i + 3], s);
-  }
-  // lane g's dwords are rows r = 4 g .. 4 g + 3 of every group
-  quad_transpose(w, g, x);
-  byte_transpose(x, w);
+  group_codes(f, fp4_scale(sb), w);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<uint32_t*>(pv + code + (tok / 4) * 256 + (4 * g + i) * 16 + (tok % 4) * 4) =
-        w[i];
-  pv[scale] = static_cast<char>(sb);
+    *reinterpret_cast<uint32_t*>(pv + code + fp4_v_code_at(tok, 4 * g + i)) = w[i];
+  pv[scale + fp4_v_scale_at(tok, g)] = static_cast<char>(sb);
 }
 
 __global__ __launch_bounds__(256) void kv_read4_kernel(
@@ -196,36 +163,19 @@ __global__ __launch_bounds__(256) void kv_read4_kernel(
   const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
   const char* const pk = pt_k[at.page];
   const char* const pv = pt_v[at.page];
-  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale + tok * 4 + g;
-  const uint4 u = *reinterpret_cast<const uint4*>(pk + code + tok * 64 + g * 16);
-  uint32_t x[4], w[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = *reinterpret_cast<const uint32_t*>(pv + code + (tok / 4) * 256 + (4 * g + i) * 16 +
-                                              (tok % 4) * 4);
-  const float sk = fp4_scale(static_cast<uint8_t>(pk[scale]));
-  const float sv = fp4_scale(static_cast<uint8_t>(pv[scale]));
+  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale;
+  const uint4 u = *reinterpret_cast<const uint4*>(pk + code + fp4_k_code_at(tok, g));
   const uint32_t c[4] = {u.x, u.y, u.z, u.w};
+  uint32_t x[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    k[t * 4 + i] = make_uint4(fp4_unpack<0>(c[i], sk), fp4_unpack<1>(c[i], sk),
-                              fp4_unpack<2>(c[i], sk), fp4_unpack<3>(c[i], sk));
-  byte_transpose(x, w);      // w[b]: rows 4 g .. 4 g + 3 of group b
-  quad_transpose(w, g, x);   // x[i]: rows 4 i .. 4 i + 3 of this lane's group
-  uint32_t lo[8], hi[8];     // dims 2 i, 2 i + 1 and 16 + 2 i, 16 + 2 i + 1
+    x[i] = *reinterpret_cast<const uint32_t*>(pv + code + fp4_v_code_at(tok, 4 * g + i));
+  const float sk = fp4_scale(static_cast<uint8_t>(pk[scale + fp4_k_scale_at(tok, g)]));
+  const float sv = fp4_scale(static_cast<uint8_t>(pv[scale + fp4_v_scale_at(tok, g)]));
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t a = fp4_unpack<0>(x[i], sv), b = fp4_unpack<1>(x[i], sv);
-    const uint32_t d = fp4_unpack<2>(x[i], sv), e = fp4_unpack<3>(x[i], sv);
-    lo[2 * i] = __builtin_amdgcn_perm(b, a, 0x05040100);
-    hi[2 * i] = __builtin_amdgcn_perm(b, a, 0x07060302);
-    lo[2 * i + 1] = __builtin_amdgcn_perm(e, d, 0x05040100);
-    hi[2 * i + 1] = __builtin_amdgcn_perm(e, d, 0x07060302);
-  }
-  v[t * 4] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-  v[t * 4 + 1] = make_uint4(lo[4], lo[5], lo[6], lo[7]);
-  v[t * 4 + 2] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-  v[t * 4 + 3] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+  for (int i = 0; i < 4; ++i) k[t * 4 + i] = code_values(c[i], sk);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[t * 4 + i] = code_values(x[i], sv);
 }
 
 // Blocks copied within the pool: one workgroup per (pair, KV head of K or V,
