@@ -21,6 +21,9 @@
 
 namespace {
 
+#ifndef BST_MID
+#define BST_MID 8192
+#endif
 constexpr int kD = 128;
 constexpr int kT = 16;
 constexpr int kSum = 2 * kD;      // bytes of a summary: hi, then lo
@@ -372,15 +375,18 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
 
 // One workgroup per (request, KV head): the top_k-th largest key by its
 // digits, then the keys above it and the first of those equal to it, in order.
-// A thread owns consecutive blocks, V of them in registers (what lies past
-// V * NT blocks is read again in every pass), so that the ranks of all take
-// one scan.  The digits start at the highest bit in which any two keys differ
-// (scores of one query differ little in their exponents; from bit 31 on, most
-// keys would meet in one counter), and end when no key is left to decide.
+// Thread t holds keys t, NT + t, ..., V of them in registers (those past
+// V * NT blocks are read again in every pass).  The digits start at the
+// highest bit in which any two keys differ (scores of one query differ little
+// in their exponents: from bit 31 on, most keys would meet in one counter) and
+// end when no key is left to decide.  Bound by its passes' barriers, not by
+// the 4 bytes a block.
 template <int NT, int V>
 __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
-  constexpr int kWaves = NT / 64;
-  __shared__ int hist[256], s_a[kWaves], s_b[kWaves], s_pick[3];
+  constexpr int kWaves = NT / 64, kRound = 64;  // chunks of NT keys ranked at a time
+  __shared__ int hist[256], s_pick[3];
+  __shared__ int s_cnt[kRound * (kWaves + 1)];  // above | equal << 16, of a chunk's wavefronts
+  __shared__ uint32_t s_bits[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b = blockIdx.x / P.H;
   const int n = context_blocks(P, b);
@@ -390,65 +396,90 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
     return;
   }
   const float* const scores = P.scores + static_cast<int64_t>(blockIdx.x) * P.max_blocks;
-  // blocks that are always taken stand above every score
-  auto key_at = [&](int i) {
-    if (i < P.n_first || i >= n - P.n_last) return 0xffffffffu;
-    const uint32_t u = __float_as_uint(scores[i] + 0.f);  // -0 as 0: they are equal
-    return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+  // the key of blocks that are always taken; no score's (it would be a NaN's)
+  constexpr uint32_t kAlways = 0xffffffffu;
+  auto key_of = [&](float score, int i) {
+    const uint32_t u = __float_as_uint(score + 0.f);  // -0 as 0: they are equal
+    const uint32_t k = u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+    return i < P.n_first || i >= n - P.n_last ? kAlways : k;
   };
-  const int per = (n + NT - 1) / NT, beg = min(n, tid * per), cnt = min(n, beg + per) - beg;
+  auto key_at = [&](int i) { return key_of(scores[i], i); };
+  const int chunks = (n + NT - 1) / NT;
   uint32_t key[V];
+  float own[V];  // loaded without a branch, all of them together
 #pragma unroll
-  for (int j = 0; j < V; ++j) key[j] = j < cnt ? key_at(beg + j) : 0;
-  auto each = [&](auto f) {
+  for (int j = 0; j < V; ++j) own[j] = scores[min(j * NT + tid, n - 1)];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const uint32_t k = key_of(own[j], j * NT + tid);
+    key[j] = j * NT + tid < n ? k : kAlways;
+  }
+  auto each = [&](auto f) {  // the keys that are to be ordered
 #pragma unroll
     for (int j = 0; j < V; ++j)
-      if (j < cnt) f(key[j], beg + j);
-    for (int j = V; j < cnt; ++j) f(key_at(beg + j), beg + j);
+      if (key[j] != kAlways) f(key[j]);
+    for (int i = V * NT + tid; i < n; i += NT) {
+      const uint32_t k = key_at(i);
+      if (k != kAlways) f(k);
+    }
   };
-  // bits in which keys differ: those that are set somewhere and clear somewhere
+  // bits in which keys differ: set in one and clear in another
   uint32_t any1 = 0, any0 = 0;
-  each([&](uint32_t k, int) {
+  each([&](uint32_t k) {
     any1 |= k;
     any0 |= ~k;
   });
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
-    any1 |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(any1), m, 64));
-    any0 |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(any0), m, 64));
-  }
+  auto either = [](uint32_t x, uint32_t y) { return x | y; };
+  auto over_wave = [&](uint32_t v) {
+    v |= dpp<kXor1>(v);
+    v |= dpp<kXor2>(v);
+    v |= dpp<kXor7>(v);
+    v |= dpp<kXor8>(v);
+    return over_rows(v, either);
+  };
+  any1 = over_wave(any1);
+  any0 = over_wave(any0);
   if (lane == 0) {
-    s_a[wave] = static_cast<int>(any1);
-    s_b[wave] = static_cast<int>(any0);
+    s_bits[0][wave] = any1;
+    s_bits[1][wave] = any0;
   }
+  for (int i = tid; i < 256; i += NT) hist[i] = 0;
   __syncthreads();
-  any1 = any0 = 0;
+#pragma unroll
   for (int w = 0; w < kWaves; ++w) {
-    any1 |= static_cast<uint32_t>(s_a[w]);
-    any0 |= static_cast<uint32_t>(s_b[w]);
+    any1 |= s_bits[0][w];
+    any0 |= s_bits[1][w];
   }
   const uint32_t differ = any1 & any0;
-  // (all equal: the keys at and above any1 & ~any0, none above)
-  uint32_t least = any1 & ~any0;  // the bits that all share; then the decided ones
-  int need = P.top_k;             // of the keys whose decided bits equal least's
   int top = differ ? 32 - __clz(static_cast<int>(differ)) : 0;  // undecided bits
-  least = top == 32 ? 0 : least >> top << top;
-  bool open = true;
+  // the decided bits of the last key that is taken; at first those all share
+  uint32_t least = top == 32 ? 0 : (any1 & ~any0) >> top << top;
+  // how many are taken of the keys with these bits (n > top_k: the first and
+  // the last blocks are apart)
+  int need = P.top_k - P.n_first - P.n_last;
+  bool open = need > 0;
   while (open && top > 0) {
     const int shift = max(0, top - 8);
     const uint32_t digit = (1u << (top - shift)) - 1;
-    for (int i = tid; i < 256; i += NT) hist[i] = 0;
-    __syncthreads();
-    each([&](uint32_t k, int) {
-      if (top == 32 || (k ^ least) >> top == 0) atomicAdd(&hist[(k >> shift) & digit], 1);
+    each([&](uint32_t k) {
+      if (top == 32 || (k ^ least) >> top == 0) {
+        // one addition for a wavefront whose keys agree (equal scores)
+        const uint32_t d = (k >> shift) & digit;
+        const unsigned long long here = __ballot(1);
+        if (__ballot(d == static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(d))) == here) {
+          if (lane == __ffsll(here) - 1) atomicAdd(&hist[d], static_cast<int>(__popcll(here)));
+        } else {
+          atomicAdd(&hist[d], 1);
+        }
+      }
     });
     __syncthreads();
-    // the first wavefront: keys with a digit of at least 255 - 4 lane - j
-    if (wave == 0) {
+    if (wave == 0) {  // lane l: digits 255 - 4 l, ... - 3, with the keys above them
       int c[4], x = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         c[j] = hist[255 - 4 * lane - j];
+        hist[255 - 4 * lane - j] = 0;  // for the next digit
         x += c[j];
       }
       int before = x;
@@ -471,45 +502,73 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
     __syncthreads();
     least |= static_cast<uint32_t>(s_pick[0]) << shift;
     need = s_pick[1];
-    open = s_pick[2] != need;  // else all keys of this digit are taken
+    open = s_pick[2] != need;  // else every key of this digit is taken
     top = shift;
   }
-  // keys above least's decided bits are taken, and the first `need` of those
-  // that equal them
-  int above = 0, equal = 0;
-  auto place = [&](uint32_t k) { return top == 32 ? 0 : (k >> top) == (least >> top) ? 0 : k > least ? 1 : -1; };
-  each([&](uint32_t k, int) {
-    const int c = place(k);
-    above += c > 0;
-    equal += c == 0;
-  });
-  __syncthreads();  // s_a and s_b are free again
-  int x = above, y = equal;
+  // keys above `upto` are taken, and the first `need` from least to there
+  const uint32_t upto = P.top_k == P.n_first + P.n_last ? kAlways - 1
+                        : least | (top >= 32 ? 0xffffffffu : (1u << top) - 1);
+  if (P.top_k == P.n_first + P.n_last) least = kAlways;
+  int above0 = 0, equal0 = 0;  // before this round
+  for (int c0 = 0; c0 < chunks; c0 += kRound) {
+    const int m = min(kRound, chunks - c0);
+    // lane j: this wavefront's 64 blocks of chunk j that are above, and equal
+    unsigned long long gt = 0, eq = 0;
+    auto mark = [&](int j, uint32_t k, bool in) {  // all lanes together
+      const bool more = in && (k > upto || k == kAlways);
+      const unsigned long long x = __ballot(more), y = __ballot(in && !more && k >= least);
+      gt = lane == j ? x : gt;
+      eq = lane == j ? y : eq;
+    };
+    if (c0 == 0) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int u = __shfl_up(x, d, 64), v = __shfl_up(y, d, 64);
-    if (lane >= d) {
-      x += u;
-      y += v;
+      for (int j = 0; j < V; ++j) mark(j, key[j], j * NT + tid < n);
+    }
+    for (int j = c0 == 0 ? V : 0; j < m; ++j) {
+      const int i = (c0 + j) * NT + tid;
+      mark(j, key_at(min(i, n - 1)), i < n);
+    }
+    if (c0 > 0) __syncthreads();  // s_cnt is free again
+    s_cnt[lane * (kWaves + 1) + wave] = __popcll(gt) | __popcll(eq) << 16;
+    __syncthreads();
+    // what stands before: in the chunk, then in the chunks before it
+    int x = 0, y = 0, own_x = 0, own_y = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = s_cnt[lane * (kWaves + 1) + w];
+      own_x = w == wave ? x : own_x;
+      own_y = w == wave ? y : own_y;
+      x += c & 0xffff;
+      y += c >> 16;
+    }
+    int sx = x, sy = y;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int u = __shfl_up(sx, d, 64), v = __shfl_up(sy, d, 64);
+      if (lane >= d) {
+        sx += u;
+        sy += v;
+      }
+    }
+    own_x += above0 + sx - x;
+    own_y += equal0 + sy - y;
+    above0 += __builtin_amdgcn_readlane(sx, 63);
+    equal0 += __builtin_amdgcn_readlane(sy, 63);
+    // the words of which something is taken, one by one, a lane a block
+    const unsigned long long below = (1ull << lane) - 1;
+    for (unsigned long long words = __ballot(gt || (eq && own_y < need)); words; words &= words - 1) {
+      const int j = __ffsll(words) - 1;
+      auto lane_of = [&](unsigned long long v) {
+        return static_cast<unsigned long long>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), j)) << 32 |
+               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), j));
+      };
+      const unsigned long long g = lane_of(gt), q = lane_of(eq);
+      const int a = __builtin_amdgcn_readlane(own_x, j) + static_cast<int>(__popcll(g & below));
+      const int e = __builtin_amdgcn_readlane(own_y, j) + static_cast<int>(__popcll(q & below));
+      if ((g >> lane & 1) || ((q >> lane & 1) && e < need))
+        sel[a + min(e, need)] = (c0 + j) * NT + tid;
     }
   }
-  if (lane == 63) {
-    s_a[wave] = x;
-    s_b[wave] = y;
-  }
-  __syncthreads();
-  x -= above;
-  y -= equal;
-  for (int w = 0; w < wave; ++w) {
-    x += s_a[w];
-    y += s_b[w];
-  }
-  each([&](uint32_t k, int i) {
-    const int c = place(k);
-    if (c > 0 || (c == 0 && y < need)) sel[x + min(y, need)] = i;
-    x += c > 0;
-    y += c == 0;
-  });
 }
 
 }  // namespace
@@ -601,8 +660,10 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   const dim3 rows(static_cast<unsigned>(B) * H);
   if (max_blocks <= 2048)
     hipLaunchKernelGGL((select_blocks_kernel<256, 8>), rows, dim3(256), 0, s, P);
+  else if (max_blocks <= BST_MID)
+    hipLaunchKernelGGL((select_blocks_kernel<512, 16>), rows, dim3(512), 0, s, P);
   else
-    hipLaunchKernelGGL((select_blocks_kernel<1024, 8>), rows, dim3(1024), 0, s, P);
+    hipLaunchKernelGGL((select_blocks_kernel<1024, 16>), rows, dim3(1024), 0, s, P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }
