@@ -174,7 +174,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     float vf[8];
-    unpack8(MASKED ? live(vb[u], valid[u]) : vb[u], vf);
+    unpack8(vb[u], vf);
 #pragma unroll
     for (int j = 0; j < G; ++j) {
       // masked: an invalid token (score -inf) weighs 0, also while the
@@ -298,7 +298,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
       lh[i] += p[i];
     }
     bcast_groups<G>(p, pj);
-    unpack8(MASKED ? live(vb[u], valid[u]) : vb[u], vf);
+    unpack8(vb[u], vf);
 #pragma unroll
     for (int j = 0; j < G; ++j)
 #pragma unroll
@@ -482,6 +482,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
       for (int u = 0; u < kUnroll; ++u)
         all_ok = all_ok && (SEL ? row[i + u] >= 0 && row[i + u] < P.nb && s_tok[i + u] == kT
                                 : valid[u]);
+      if constexpr (SEL) {  // a partial block may stand anywhere
+        if (!all_ok)
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) vb[u] = live(vb[u], valid[u]);
+      }
       auto next_k = [&] {
         if (more)
 #pragma unroll
@@ -523,6 +528,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
         valid[u] = ok && ts < s_tok[min(i + u, nbp - 1)];
       else
         valid[u] = ok && (blk_beg + i + u) * kT + ts < L;
+      vb[u] = live(vb[u], valid[u]);
     }
     if constexpr (kHD)
       consume_hd<G, kUnroll, true>(query, kb, vb, valid, sc2, b0, b1, mh, lh, acc, none);
