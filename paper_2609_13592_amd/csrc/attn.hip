@@ -51,9 +51,13 @@ __device__ __forceinline__ void unpack8(const uint4& u, float* f) {
   f[6] = lo_bf16(u.w); f[7] = hi_bf16(u.w);
 }
 
-__device__ __forceinline__ uint4 load_block(const char* base, bool ok, uint32_t off) {
+// A lane's 16 bytes of a head-block of which the first `bytes` are read: what
+// lies behind (tokens past the context, or all of a block outside the pool)
+// comes as zeros, whatever memory holds there, so that a probability of 0
+// never meets an infinity or a NaN.
+__device__ __forceinline__ uint4 load_block(const char* base, int bytes, uint32_t off) {
   const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<char*>(base), 0, ok ? kT * kD * 2 : 0, 0x00020000);
+      const_cast<char*>(base), 0, bytes, 0x00020000);
   auto v = __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 2);
   return *reinterpret_cast<uint4*>(&v);
 }
@@ -132,8 +136,7 @@ __device__ __forceinline__ void slot_merge(float* m, float* l, float (*acc)[8]) 
   merge_state<G>(m, l, acc, m2, l2, a2);
 }
 
-// V of a token that does not count: zeros, whatever its slot holds (its
-// probability 0 must not meet an infinity or a NaN there).
+// V of a token that does not count: zeros, whatever its slot holds.
 __device__ __forceinline__ uint4 live(const uint4& v, bool valid) {
   return make_uint4(valid ? v.x : 0, valid ? v.y : 0, valid ? v.z : 0, valid ? v.w : 0);
 }
@@ -344,6 +347,8 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
 // 302 of the kernel that kept every head's score in every lane and the queries
 // in registers left one, and took 41 us for 8 requests of 2048 tokens with 64 /
 // 8 heads, 149 us for 32 of 512..4096, against 27.5 and 96).
+// (Over selected blocks two as well: clearing a masked group's V makes three
+// spill, 16 lists of 64 blocks 49 -> 64 us.)
 #ifndef BOOST_ATTN_WAVES
 #define BOOST_ATTN_WAVES 3
 #endif
@@ -351,7 +356,7 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
 // list's partial block may stand anywhere, so tokens are counted per block).
 template <int G, bool WAVE, bool SEL>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
-    G == 8 ? 2 : BOOST_ATTN_WAVES))) void attn_partition(AttnParams P) {
+    G == 8 || SEL ? 2 : BOOST_ATTN_WAVES))) void attn_partition(AttnParams P) {
   constexpr int kUnroll = G == 8 ? BOOST_ATTN_UNROLL8 : BOOST_ATTN_UNROLL;  // blocks in flight
   __shared__ float s_ml[4][G][2];
   __shared__ float s_acc[4][G][kD];
@@ -449,16 +454,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
     host = byte >= P.host_from;
     return host ? byte - P.host_from : byte;
   };
-  auto fetch_k = [&](int bi, uint4& kq) {
+  // bytes of block bi that are read: its tokens inside the context (of a
+  // list's blocks all, cleared where a group is masked: the bound's way
+  // through LDS would hold up every load, 16 lists of 64 blocks 48.9 -> 52 us)
+  auto bytes_of = [&](int bi, bool last) {
+    return (!SEL && last ? min(kT, L - (blk_beg + bi) * kT) : kT) * kD * 2;
+  };
+  auto fetch_k = [&](int bi, uint4& kq, bool last = false) {
     bool ok, host;
     const uint64_t off = where(bi, ok, host);
-    kq = load_block((host ? P.k_host : P.k_hbm) + off, ok, lane_off);
+    kq = load_block((host ? P.k_host : P.k_hbm) + off, ok ? bytes_of(bi, last) : 0, lane_off);
     return ok;
   };
-  auto fetch_v = [&](int bi, uint4& vq) {
+  auto fetch_v = [&](int bi, uint4& vq, bool last = false) {
     bool ok, host;
     const uint64_t off = where(bi, ok, host);
-    vq = load_block((host ? P.v_host : P.v_hbm) + off, ok, lane_off);
+    vq = load_block((host ? P.v_host : P.v_hbm) + off, ok ? bytes_of(bi, last) : 0, lane_off);
   };
   auto none = [] {};
   // Full groups of kUnroll blocks, software-pipelined across K and V: the
@@ -521,14 +532,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
     bool valid[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const bool ok = i + u < nbp && fetch_k(i + u, kb[u]);
-      if (i + u < nbp) fetch_v(i + u, vb[u]);
+      const bool ok = i + u < nbp && fetch_k(i + u, kb[u], true);
+      if (i + u < nbp) fetch_v(i + u, vb[u], true);
       if (i + u >= nbp) kb[u] = vb[u] = make_uint4(0, 0, 0, 0);
       if constexpr (SEL)
         valid[u] = ok && ts < s_tok[min(i + u, nbp - 1)];
       else
         valid[u] = ok && (blk_beg + i + u) * kT + ts < L;
-      vb[u] = live(vb[u], valid[u]);
+      if constexpr (SEL) vb[u] = live(vb[u], valid[u]);
     }
     if constexpr (kHD)
       consume_hd<G, kUnroll, true>(query, kb, vb, valid, sc2, b0, b1, mh, lh, acc, none);
