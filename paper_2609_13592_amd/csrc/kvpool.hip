@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 #include "kvfmt.h"
 #include "runtime.h"
@@ -56,25 +57,12 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
   v[t] = *reinterpret_cast<const uint4*>(pt_v[page] + in);
 }
 
-// ---- 4 bits: one lane per (token, head, group of 32 dims).  Bound by the
-// bytes: 256 in and 68 out per row (or the reverse).
-
-// 32 bf16 values (64 bytes at src) as floats, and their scale byte.
-__device__ __forceinline__ uint32_t load_group(const uint4* src, float* f) {
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint4 u = src[i];
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      amax = max(amax, max((w[j] << 16) & 0x7fff0000u, w[j] & 0x7fff0000u));
-      f[8 * i + 2 * j] = __uint_as_float(w[j] << 16);
-      f[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    }
-  }
-  return bst::fp4_scale_byte(amax);
-}
+// ---- 4 bits.  A workgroup takes 16 rows in a row (a prompt's tokens of one
+// block, mostly) of one KV head, a lane 8 dims: 16 bytes in and a dword of
+// codes out for K and V each, or the reverse; a quad of lanes shares a scale.
+// Bound by the bytes, 512 and 136 a row: whole lines of the rows, and the
+// head-block's lines put together in one L2.
+constexpr int kRows4 = 16;
 
 // Slot of row i: given (slots), or that of request i's token at pos[i] (a
 // position or a block outside the table or the pool: -1).
@@ -98,84 +86,92 @@ __device__ __forceinline__ int64_t slot_of(const RowSlot& r, int64_t i, int nb) 
   return slot < static_cast<int64_t>(nb) * bst::kFp4Tok ? slot : -1;
 }
 
-// The codes of 32 values, eight to a dword.
-__device__ __forceinline__ void group_codes(const float* f, float s, uint32_t* w) {
+// Eight bf16 values in 4 bits; sb: their group's scale byte, found over the
+// quad of lanes that hold it.
+__device__ __forceinline__ uint32_t codes_of(const uint4& u, uint32_t& sb) {
   using namespace bst;
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  uint32_t amax = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    w[i] = fp4_pack<0>(0u, f[8 * i], f[8 * i + 1], s);
-    w[i] = fp4_pack<1>(w[i], f[8 * i + 2], f[8 * i + 3], s);
-    w[i] = fp4_pack<2>(w[i], f[8 * i + 4], f[8 * i + 5], s);
-    w[i] = fp4_pack<3>(w[i], f[8 * i + 6], f[8 * i + 7], s);
-  }
+  for (int i = 0; i < 4; ++i)
+    amax = max(amax, max((w[i] << 16) & 0x7fff0000u, w[i] & 0x7fff0000u));
+  auto far = [&](auto ctrl) {
+    return static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(
+        static_cast<int>(amax), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  amax = max(amax, far(std::integral_constant<int, 0xb1>{}));  // the lane xor 1
+  amax = max(amax, far(std::integral_constant<int, 0x4e>{}));  // xor 2
+  sb = fp4_scale_byte(amax);
+  const float s = fp4_scale(sb);
+  auto lo = [&](int i) { return __uint_as_float(w[i] << 16); };
+  auto hi = [&](int i) { return __uint_as_float(w[i] & 0xffff0000u); };
+  uint32_t c = fp4_pack<0>(0u, lo(0), hi(0), s);
+  c = fp4_pack<1>(c, lo(1), hi(1), s);
+  c = fp4_pack<2>(c, lo(2), hi(2), s);
+  return fp4_pack<3>(c, lo(3), hi(3), s);
 }
 
-// Eight bf16 values of a dword of codes.
-__device__ __forceinline__ uint4 code_values(uint32_t c, float s) {
+// ... and back.
+__device__ __forceinline__ uint4 values_of(uint32_t c, uint32_t sb) {
   using namespace bst;
+  const float s = fp4_scale(sb);
   return make_uint4(fp4_unpack<0>(c, s), fp4_unpack<1>(c, s), fp4_unpack<2>(c, s),
                     fp4_unpack<3>(c, s));
 }
 
-__global__ __launch_bounds__(256) void kv_write4_kernel(
-    const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v, RowSlot rows,
-    const uint4* __restrict__ k, const uint4* __restrict__ v, int n, int H, int nb) {
+// Where lane r (of 16) of a row finds its dwords and scales.
+struct Row4 {
+  char *k, *v, *ks, *vs;
+};
+__device__ __forceinline__ Row4 row4(const char* const* pt_k, const char* const* pt_v,
+                                     int64_t slot, int h, int nb, int r) {
   using namespace bst;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (t >= static_cast<int64_t>(n) * H * 4) return;
-  const int g = static_cast<int>(t & 3);
-  const int64_t th = t >> 2;
-  const int h = static_cast<int>(th % H);
-  const int64_t slot = slot_of(rows, th / H, nb);
-  if (slot < 0) return;
   const int tok = static_cast<int>(slot % kFp4Tok);
   const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
   char* const pk = const_cast<char*>(pt_k[at.page]);
   char* const pv = const_cast<char*>(pt_v[at.page]);
   const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale;
-  float f[32];
-  uint32_t sb = load_group(k + t * 4, f), w[4];
-  group_codes(f, fp4_scale(sb), w);
-  *reinterpret_cast<uint4*>(pk + code + fp4_k_code_at(tok, g)) =
-      make_uint4(w[0], w[1], w[2], w[3]);
-  pk[scale + fp4_k_scale_at(tok, g)] = static_cast<char>(sb);
-  sb = load_group(v + t * 4, f);
-  group_codes(f, fp4_scale(sb), w);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    *reinterpret_cast<uint32_t*>(pv + code + fp4_v_code_at(tok, 4 * g + i)) = w[i];
-  pv[scale + fp4_v_scale_at(tok, g)] = static_cast<char>(sb);
+  return {pk + code + fp4_k_code_at(tok, r / 4) + r % 4 * 4, pv + code + fp4_v_code_at(tok, r),
+          pk + scale + fp4_k_scale_at(tok, r / 4), pv + scale + fp4_v_scale_at(tok, r / 4)};
 }
 
-__global__ __launch_bounds__(256) void kv_read4_kernel(
+__global__ __launch_bounds__(16 * kRows4) void kv_write4_kernel(
+    const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v, RowSlot rows,
+    const uint4* __restrict__ k, const uint4* __restrict__ v, int n, int H, int nb) {
+  const int r = threadIdx.x & 15, h = blockIdx.x % H;
+  const int64_t i = static_cast<int64_t>(blockIdx.x / H) * kRows4 + (threadIdx.x >> 4);
+  if (i >= n) return;  // whole rows of lanes
+  const int64_t slot = slot_of(rows, i, nb);
+  if (slot < 0) return;
+  const int64_t at = (i * H + h) * 16 + r;
+  const uint4 uk = k[at], uv = v[at];
+  const Row4 to = row4(pt_k, pt_v, slot, h, nb, r);
+  uint32_t sk, sv;
+  const uint32_t ck = codes_of(uk, sk), cv = codes_of(uv, sv);
+  *reinterpret_cast<uint32_t*>(to.k) = ck;
+  *reinterpret_cast<uint32_t*>(to.v) = cv;
+  if (r % 4 == 0) {
+    *to.ks = static_cast<char>(sk);
+    *to.vs = static_cast<char>(sv);
+  }
+}
+
+__global__ __launch_bounds__(16 * kRows4) void kv_read4_kernel(
     const char* const* __restrict__ pt_k, const char* const* __restrict__ pt_v,
     const int32_t* __restrict__ slots, uint4* __restrict__ k, uint4* __restrict__ v, int n, int H,
     int nb) {
-  using namespace bst;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-  if (t >= static_cast<int64_t>(n) * H * 4) return;
-  const int g = static_cast<int>(t & 3);
-  const int64_t th = t >> 2;
-  const int h = static_cast<int>(th % H);
-  const int64_t slot = slot_of(RowSlot{slots, nullptr, nullptr, 0}, th / H, nb);
+  const int r = threadIdx.x & 15, h = blockIdx.x % H;
+  const int64_t i = static_cast<int64_t>(blockIdx.x / H) * kRows4 + (threadIdx.x >> 4);
+  if (i >= n) return;
+  const int64_t slot = slot_of(RowSlot{slots, nullptr, nullptr, 0}, i, nb);
   if (slot < 0) return;
-  const int tok = static_cast<int>(slot % kFp4Tok);
-  const Fp4At at = fp4_at(h, static_cast<int>(slot / kFp4Tok), nb);
-  const char* const pk = pt_k[at.page];
-  const char* const pv = pt_v[at.page];
-  const uint32_t code = at.idx * kFp4Code, scale = kFp4ScaleAt + at.idx * kFp4Scale;
-  const uint4 u = *reinterpret_cast<const uint4*>(pk + code + fp4_k_code_at(tok, g));
-  const uint32_t c[4] = {u.x, u.y, u.z, u.w};
-  uint32_t x[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    x[i] = *reinterpret_cast<const uint32_t*>(pv + code + fp4_v_code_at(tok, 4 * g + i));
-  const float sk = fp4_scale(static_cast<uint8_t>(pk[scale + fp4_k_scale_at(tok, g)]));
-  const float sv = fp4_scale(static_cast<uint8_t>(pv[scale + fp4_v_scale_at(tok, g)]));
-#pragma unroll
-  for (int i = 0; i < 4; ++i) k[t * 4 + i] = code_values(c[i], sk);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[t * 4 + i] = code_values(x[i], sv);
+  const int64_t at = (i * H + h) * 16 + r;
+  const Row4 from = row4(pt_k, pt_v, slot, h, nb, r);
+  const uint32_t ck = *reinterpret_cast<const uint32_t*>(from.k);
+  const uint32_t cv = *reinterpret_cast<const uint32_t*>(from.v);
+  const uint32_t sk = static_cast<uint8_t>(*from.ks), sv = static_cast<uint8_t>(*from.vs);
+  k[at] = values_of(ck, sk);
+  v[at] = values_of(cv, sv);
 }
 
 // Blocks copied within the pool: one workgroup per (pair, KV head of K or V,
@@ -277,9 +273,9 @@ int kv_write4(const boost_kv_pool* p, int layer, const int32_t* slots, const int
   const char* const *pk, * const *pv;
   if (int rc = kv_layer(p, layer, &pk, &pv)) return rc;
   const int H = static_cast<int>(p->cfg.kv_heads);
-  const int64_t grid = (static_cast<int64_t>(n) * H * 4 + 255) / 256;
+  const int64_t grid = (static_cast<int64_t>(n) + kRows4 - 1) / kRows4 * H;
   if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "n=%d: grid too large", n);
-  hipLaunchKernelGGL(kv_write4_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
+  hipLaunchKernelGGL(kv_write4_kernel, dim3(static_cast<unsigned>(grid)), dim3(16 * kRows4), 0,
                      static_cast<hipStream_t>(stream), pk, pv,
                      RowSlot{slots, tables, positions, max_blocks}, static_cast<const uint4*>(k),
                      static_cast<const uint4*>(v), n, H, static_cast<int>(p->geom.nb));
@@ -520,12 +516,13 @@ int boost_kv_read(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int32
     return fail(BOOST_EINVAL, "k and v must be 16-byte aligned");
   const int H = static_cast<int>(p->cfg.kv_heads), D = static_cast<int>(p->cfg.head_dim);
   const bool fp4 = p->format == BOOST_KV_FP4;
-  const int64_t grid = (static_cast<int64_t>(n) * H * (fp4 ? 4 : D / 8) + 255) / 256;
+  const int64_t grid = fp4 ? (static_cast<int64_t>(n) + kRows4 - 1) / kRows4 * H
+                           : (static_cast<int64_t>(n) * H * (D / 8) + 255) / 256;
   if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "n=%d: grid too large", n);
   const dim3 g(static_cast<unsigned>(grid));
   const auto s = static_cast<hipStream_t>(stream);
   if (fp4)
-    hipLaunchKernelGGL(kv_read4_kernel, g, dim3(256), 0, s, pk, pv, slots, static_cast<uint4*>(k),
+    hipLaunchKernelGGL(kv_read4_kernel, g, dim3(16 * kRows4), 0, s, pk, pv, slots, static_cast<uint4*>(k),
                        static_cast<uint4*>(v), n, H, static_cast<int>(p->geom.nb));
   else
     hipLaunchKernelGGL(kv_read_kernel, g, dim3(256), 0, s, pk, pv, slots, static_cast<uint4*>(k),
