@@ -856,7 +856,8 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
        std::max(part_min, std::min(kPartMax, (max_blocks + want_parts - 1) / want_parts))});
   P.part_blocks = std::max(P.part_blocks, 4);
   // a 4-bit context of one partition needs no merge
-  if (fp4 && max_blocks <= kOneBlocks) P.part_blocks = std::max(max_blocks, 4);
+  if (fp4 && max_blocks <= (B * H < ctx->n_cu / 2 ? kOneFew : kOneMany))
+    P.part_blocks = std::max(max_blocks, 4);
   P.n_parts = (max_blocks + P.part_blocks - 1) / P.part_blocks;
   P.max_parts = max_parts > 0 ? max_parts : P.n_parts;
   if (P.n_parts > P.max_parts) return fail(BOOST_EINVAL, "partition scratch too small");
@@ -874,7 +875,7 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   int rc;
   if (fp4) {
     if (G > 8) return fail(BOOST_EINVAL, "Hq/H=%d above 8", G);
-    rc = launch_fp4(P, s);
+    rc = launch_fp4(P, ctx->n_cu, s);
     if (P.n_parts == 1) return rc;
   } else {
     switch (G) {

@@ -71,13 +71,15 @@ struct Block4 {
   int tok;      // tokens that count
 };
 
-// EIGHT: more than four query heads per KV head.  ONE: no context has more
+// EIGHT: more than four query heads per KV head.  kOne: no context has more
 // than one partition: a workgroup for every (KV head, request), empty ones too.
+// W wavefronts (kWave and kGroup: 4, as the item search has it).
 enum class Items { kWave, kGroup, kOne };
-template <bool EIGHT, Items ITEMS, bool SEL>
-__global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
-  __shared__ float s_acc[4][8][kAccRow];  // heads (EIGHT), else 4 heads of each part
-  __shared__ float s_ml[4][8][2];
+template <bool EIGHT, Items ITEMS, bool SEL, int W>
+__global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
+  static_assert(ITEMS == Items::kOne || 64 * W == kThreads, "item search");
+  __shared__ float s_acc[W][8][kAccRow];  // heads (EIGHT), else 4 heads of each part
+  __shared__ float s_ml[W][8][2];
   __shared__ int32_t row[kMaxPartBlocks];    // the partition's pool blocks
   __shared__ int32_t s_tok[kMaxPartBlocks];  // and their tokens that count
   __shared__ int s_red[4], s_pick[5];
@@ -100,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
   const int blk_beg = part * P.part_blocks;
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
   const bool whole = n_blk <= P.part_blocks;
-  for (int i = tid; i < nbp; i += kThreads) {
+  for (int i = tid; i < nbp; i += 64 * W) {
     int tok;
     int32_t blk;
     if constexpr (SEL) {
@@ -256,16 +258,17 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
     // The next pair's loads are out while a pair is computed.  They are issued
     // without a branch (past the end: the last block again, from the caches),
     // so that the waits can count them.
+    constexpr int kStep = 2 * W;
     Block4 a0, a1, b0, b1;
     fetch(2 * wave, a0);
     fetch(2 * wave + 1, a1);
-    for (int i = 2 * wave; i < nbp; i += 16) {
-      fetch(i + 8, b0);
-      fetch(i + 9, b1);
+    for (int i = 2 * wave; i < nbp; i += 2 * kStep) {
+      fetch(i + kStep, b0);
+      fetch(i + kStep + 1, b1);
       consume(a0, a1);
-      if (i + 8 >= nbp) break;  // uniform over the wavefront
-      fetch(i + 16, a0);
-      fetch(i + 17, a1);
+      if (i + kStep >= nbp) break;  // uniform over the wavefront
+      fetch(i + 2 * kStep, a0);
+      fetch(i + 2 * kStep + 1, a1);
       consume(b0, b1);
     }
   }
@@ -284,14 +287,14 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
   __syncthreads();
   // four dims of a head per thread: the wavefronts in order, each one's parts
   // from the largest, at the common maximum
-  for (int e = tid; e < G * (kD / 4); e += kThreads) {
+  for (int e = tid; e < G * (kD / 4); e += 64 * W) {
     const int j = e / (kD / 4), d4 = e % (kD / 4) * 4;
     float M = -kLowest, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ml[w][j][0]);
+    for (int w = 0; w < W; ++w) M = fmaxf(M, s_ml[w][j][0]);
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float c = __builtin_amdgcn_exp2f(s_ml[w][j][0] - M);
       sum += s_ml[w][j][1] * c;
       f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][j][d4]);
@@ -323,22 +326,31 @@ __global__ __launch_bounds__(kThreads) void attn4_partition(AttnParams P) {
   }
 }
 
-template <bool EIGHT, Items ITEMS>
+template <bool EIGHT, Items ITEMS, int W>
 void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
   if (P.sel)
-    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, true>), dim3(grid), dim3(kThreads), 0, s, P);
+    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, true, W>), dim3(grid), dim3(64 * W), 0, s, P);
   else
-    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, false>), dim3(grid), dim3(kThreads), 0, s, P);
+    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, false, W>), dim3(grid), dim3(64 * W), 0, s,
+                       P);
 }
 
 template <bool EIGHT>
-void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
-  if (P.n_parts == 1)
-    launch<EIGHT, Items::kOne>(P, grid, s);
-  else if (P.B <= 64)
-    launch<EIGHT, Items::kWave>(P, grid, s);
-  else
-    launch<EIGHT, Items::kGroup>(P, grid, s);
+void launch(const AttnParams& P, unsigned grid, int n_cu, hipStream_t s) {
+  if (P.n_parts == 1) {
+    // a workgroup alone on its compute unit: a pair is one chain of products,
+    // maximum, exponentials and products, 83 ns a block with four wavefronts,
+    // 61 with eight (57 with 16: the unit's bandwidth); 32 requests of 1500
+    // tokens 12.4 us with eight and 13.9 with four, 64 of 1000 17.2 and 15.9
+    if (P.B * P.H <= n_cu)
+      launch<EIGHT, Items::kOne, 8>(P, grid, s);
+    else
+      launch<EIGHT, Items::kOne, 4>(P, grid, s);
+  } else if (P.B <= 64) {
+    launch<EIGHT, Items::kWave, 4>(P, grid, s);
+  } else {
+    launch<EIGHT, Items::kGroup, 4>(P, grid, s);
+  }
 }
 
 }  // namespace
@@ -346,13 +358,13 @@ void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
 namespace bst {
 namespace attn {
 
-int launch_fp4(AttnParams& P, hipStream_t s) {
+int launch_fp4(AttnParams& P, int n_cu, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
   if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "grid too large");
   if (P.Hq / P.H <= 4)
-    launch<false>(P, static_cast<unsigned>(grid), s);
+    launch<false>(P, static_cast<unsigned>(grid), n_cu, s);
   else
-    launch<true>(P, static_cast<unsigned>(grid), s);
+    launch<true>(P, static_cast<unsigned>(grid), n_cu, s);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

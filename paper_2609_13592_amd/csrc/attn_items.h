@@ -21,13 +21,12 @@ constexpr int kT = 16;           // tokens per block
 #ifndef BOOST_ATTN_ITEMS4
 #define BOOST_ATTN_ITEMS4 768
 #endif
-// 4-bit contexts of up to this many blocks stay whole: a launch without a
-// merge (one request of 301 tokens 4.9 us, cut in five 7.2; of 800 tokens 7.4
-// either way, of 1000 8.1 and 7.4; 64 requests of 1000 15.7 and 21.9)
-#ifndef BST_ONE
-#define BST_ONE 50
-#endif
-constexpr int kOneBlocks = BST_ONE;
+// 4-bit contexts of up to this many blocks stay whole, a launch without a
+// merge: where their workgroups leave half of the compute units empty (one
+// request of 301 tokens 4.9 us, cut in five 7.2; of 1000 7.6 and 7.4), and
+// where they do not (16 requests of 2000 tokens 12.7 and 14.5, of 4000 21.5 and
+// 20.4; 64 of 2000 27.4 and 31.5).
+constexpr int kOneFew = 60, kOneMany = 160;
 constexpr int kMaxPartBlocks = 256;         // blocks per partition, at most
 static_assert(kMaxPartBlocks <= kThreads, "one thread per partition size");
 // A work item of fewer than 16 blocks spends as long on its start (q loads)
@@ -304,7 +303,7 @@ __device__ __forceinline__ int32_t selected(const AttnParams& P, int b, int g, i
 // The kernels of a 4-bit pool: launches the partitions (any Hq / H up to 8).
 // Contexts of one partition are finished there; if none has more (n_parts 1),
 // empty ones too, and there is nothing to merge.
-int launch_fp4(AttnParams& P, hipStream_t s);
+int launch_fp4(AttnParams& P, int n_cu, hipStream_t s);
 
 }  // namespace attn
 }  // namespace bst

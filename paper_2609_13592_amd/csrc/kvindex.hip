@@ -4,7 +4,8 @@
 // Summary of a head-block: for every dim the largest and the smallest key of
 // its live tokens, outwards in whole steps of 2^e, e the smallest (>= -126)
 // with max|k| <= 127 * 2^e:
-//   hi_d = ceil(max_t k_td / 2^e)   lo_d = floor(min_t k_td / 2^e)   (int8)
+//   hi_d = ceil(max_t k_td / 2^e)   lo_d = floor(min_t k_td / 2^e)
+// kept as int8 hi_d and -lo_d, so that both meet magnitudes of q8 below.
 // Score of a block for a query head: q8 = round(q / 2^eq) (the same rule for
 // eq, ties to even, at most 127), 2^(e + eq) sum_d max(q8_d hi_d, q8_d lo_d),
 // an upper bound of q8 . k over the block's tokens; for a KV head the largest
@@ -26,7 +27,7 @@ namespace {
 #endif
 constexpr int kD = 128;
 constexpr int kT = 16;
-constexpr int kSum = 2 * kD;      // bytes of a summary: hi, then lo
+constexpr int kSum = 2 * kD;      // bytes of a summary: hi, then -lo
 constexpr int kNotFinite = 127;   // exponent byte of a block with an inf or NaN key
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
@@ -178,8 +179,8 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int ch
       const uint32_t hx = values_of(mx[0]), hn = values_of(mn[0]);
       const char2 hi = {static_cast<signed char>(ceilf(lo_bf16(hx) * scale)),
                         static_cast<signed char>(ceilf(hi_bf16(hx) * scale))};
-      const char2 lo = {static_cast<signed char>(floorf(lo_bf16(hn) * scale)),
-                        static_cast<signed char>(floorf(hi_bf16(hn) * scale))};
+      const char2 lo = {static_cast<signed char>(ceilf(lo_bf16(hn) * -scale)),
+                        static_cast<signed char>(ceilf(hi_bf16(hn) * -scale))};
       int8_t* const o = out + 32 * qd + 2 * r;
       *reinterpret_cast<char2*>(o) = bad ? char2{0, 0} : hi;
       *reinterpret_cast<char2*>(o + kD) = bad ? char2{0, 0} : lo;
@@ -227,9 +228,9 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int ch
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t v = values_of(qd == 0 ? mx[j] : mn[j]);
-          const float x = lo_bf16(v) * scale, y = hi_bf16(v) * scale;
-          const int p = static_cast<int>(qd == 0 ? ceilf(x) : floorf(x));
-          const int q = static_cast<int>(qd == 0 ? ceilf(y) : floorf(y));
+          const float sg = qd == 0 ? scale : -scale;
+          const int p = static_cast<int>(ceilf(lo_bf16(v) * sg));
+          const int q = static_cast<int>(ceilf(hi_bf16(v) * sg));
           w[j / 2] |= ((static_cast<uint32_t>(p) & 255u) | (static_cast<uint32_t>(q) & 255u) << 8)
                       << (16 * (j % 2));
         }
@@ -259,19 +260,23 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
 
 // Scores of 16-block tiles, four to a wavefront: rows are blocks, columns the
 // KV head's query heads, the 256 products of a pair in four 16x16x64 integer
-// products (hi against the positive part of q8, lo against the negative).
-// Bound by the summaries' bytes; the loads of all four tiles are out together,
-// and q is rounded while they are.
+// products (hi against the positive part of q8, -lo against the magnitude of
+// the negative one).  Bound by the summaries' bytes and the chain before them
+// (lengths, block ids): the loads of all four tiles are out together, and q is
+// rounded while they are, a quarter by each wavefront.
 constexpr int kTileBlocks = 16, kTiles = 4;
 constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
 __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int chunks) {
+  // the operand of q by lane: dword w of 16 dims of step s (positive parts of
+  // the lower and the upper 64 dims, then the negative ones)
+  __shared__ uint32_t s_q[4][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
   const int chunk = blockIdx.x % chunks, bg = blockIdx.x / chunks;
   const int g = bg % P.H, b = bg / P.H;
   const int n = context_blocks(P, b);
+  if (chunk * kScoreBlocks >= n) return;  // uniform
   const int first = chunk * kScoreBlocks + wave * kTiles * kTileBlocks;
-  if (first >= n) return;  // uniform over the wavefront; no barrier follows
   const int G = P.Hq / P.H;
   const int8_t* const sum = P.sum + static_cast<int64_t>(g) * P.nb * kSum;
   const int8_t* const exps = P.exp + static_cast<int64_t>(g) * P.nb;
@@ -280,9 +285,21 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
   i32x4 a[kTiles][4];
   int e[kTiles];  // of block (row) r; -128: no such block
 #pragma unroll
-  for (int i = 0; i < kTiles; ++i) {
-    const int blk = first + i * kTileBlocks + r;
-    id[i] = table[min(blk, n - 1)];
+  for (int i = 0; i < kTiles; ++i)
+    id[i] = table[min(first + i * kTileBlocks + r, n - 1)];
+  // column r: head r (beyond G the last again), dims 16 qd .. + 15 and 64 more
+  uint32_t w[16];
+  {
+    const uint4* q = reinterpret_cast<const uint4*>(
+        P.q + (static_cast<int64_t>(b) * P.Hq + g * G + min(r, G - 1)) * kD + 16 * qd);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint4 u = q[i < 2 ? i : 6 + i];  // 64 dims are 8 uint4 further
+      w[4 * i] = u.x;
+      w[4 * i + 1] = u.y;
+      w[4 * i + 2] = u.z;
+      w[4 * i + 3] = u.w;
+    }
   }
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
@@ -294,49 +311,39 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
     e[i] = exps[id[i]];
     e[i] = ok ? e[i] : -128;
   }
-  // column r: head r (zero beyond G), dims 16 qd .. + 15 and 64 more
-  i32x4 qb[4];
-  int eq;
-  {
-    const uint4* q = reinterpret_cast<const uint4*>(
-        P.q + (static_cast<int64_t>(b) * P.Hq + g * G + min(r, G - 1)) * kD + 16 * qd);
-    uint32_t w[16], amax = 0;
+  uint32_t amax = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint4 u = q[i < 2 ? i : 6 + i];  // 64 dims are 8 uint4 further
-      w[4 * i] = u.x;
-      w[4 * i + 1] = u.y;
-      w[4 * i + 2] = u.z;
-      w[4 * i + 3] = u.w;
+  for (int i = 0; i < 16; ++i) amax = max(amax, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
+  amax = over_rows(amax, [](uint32_t x, uint32_t y) { return max(x, y); });
+  const bool none = amax >= 0x7f80;  // a query that is not finite counts as 0
+  const int eq = none ? 0 : step_exponent(amax);
+  const float step = pow2f(-eq);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {  // this wavefront's four dims of the lower and upper 64
+    uint32_t x0 = w[8 * h], x1 = w[8 * h + 1];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) {
+      x0 = wave == i ? w[8 * h + 2 * i] : x0;
+      x1 = wave == i ? w[8 * h + 2 * i + 1] : x1;
     }
+    // whole numbers up to 127 by the rule of eq; the conversion has 0 for
+    // what is below 0
+    const float f[4] = {rintf(lo_bf16(x0) * step), rintf(hi_bf16(x0) * step),
+                        rintf(lo_bf16(x1) * step), rintf(hi_bf16(x1) * step)};
+    uint32_t pos = 0, neg = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) amax = max(amax, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-    amax = over_rows(amax, [](uint32_t x, uint32_t y) { return max(x, y); });
-    const bool none = amax >= 0x7f80 || r >= G;  // a query that is not finite counts as 0
-    eq = none ? 0 : step_exponent(amax);
-    const float step = none ? 0.f : pow2f(-eq);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t pos[2], neg[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        pos[h] = neg[h] = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t x = w[4 * i + 2 * h + j / 2];
-          const float f = (j & 1 ? hi_bf16(x) : lo_bf16(x)) * step;
-          // (a NaN or infinity times 0 is a NaN: fminf and fmaxf drop it)
-          const int v = none ? 0 : static_cast<int>(fminf(fmaxf(rintf(f), -127.f), 127.f));
-          pos[h] |= (static_cast<uint32_t>(max(v, 0)) & 255u) << (8 * j);
-          neg[h] |= (static_cast<uint32_t>(min(v, 0)) & 255u) << (8 * j);
-        }
-      }
-      qb[i / 2][2 * (i % 2)] = static_cast<int>(pos[0]);
-      qb[i / 2][2 * (i % 2) + 1] = static_cast<int>(pos[1]);
-      qb[2 + i / 2][2 * (i % 2)] = static_cast<int>(neg[0]);
-      qb[2 + i / 2][2 * (i % 2) + 1] = static_cast<int>(neg[1]);
+    for (int j = 0; j < 4; ++j) {
+      pos = __builtin_amdgcn_cvt_pk_u8_f32(f[j], j, pos);
+      neg = __builtin_amdgcn_cvt_pk_u8_f32(-f[j], j, neg);
     }
+    s_q[h][lane][wave] = none ? 0 : pos;
+    s_q[2 + h][lane][wave] = none ? 0 : neg;
   }
+  __syncthreads();
+  if (first >= n) return;  // uniform over the wavefront; no barrier follows
+  i32x4 qb[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) qb[s] = *reinterpret_cast<const i32x4*>(s_q[s][lane]);
   float* const to = P.scores + (static_cast<int64_t>(b) * P.H + g) * P.max_blocks;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
@@ -355,21 +362,23 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
     const uint32_t q0 = __builtin_amdgcn_readlane(quad, 0), q1 = __builtin_amdgcn_readlane(quad, 4);
     const uint32_t q2 = __builtin_amdgcn_readlane(quad, 8), q3 = __builtin_amdgcn_readlane(quad, 12);
     const uint32_t er4 = qd == 0 ? q0 : qd == 1 ? q1 : qd == 2 ? q2 : q3;
-    float v[4];
+    float v = 0.f;
+    int ev = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int er = static_cast<int8_t>(er4 >> (8 * j));
       // the largest column (of up to 16 heads)
-      float x = r < G ? ldexpf(static_cast<float>(c[j]), er + eq) : -INFINITY;
+      float x = ldexpf(static_cast<float>(c[j]), er + eq);
       auto larger = [](float p, uint32_t q) { return fmaxf(p, __uint_as_float(q)); };
       x = larger(x, dpp<kXor1>(__float_as_uint(x)));
       x = larger(x, dpp<kXor2>(__float_as_uint(x)));
       x = larger(x, dpp<kXor7>(__float_as_uint(x)));
       x = larger(x, dpp<kXor8>(__float_as_uint(x)));
-      v[j] = er == -128 ? -INFINITY : er == kNotFinite ? INFINITY : x;
+      v = r == j ? x : v;
+      ev = r == j ? er : ev;
     }
     if (r < 4 && row0 + 4 * qd + r < n)
-      to[row0 + 4 * qd + r] = r == 0 ? v[0] : r == 1 ? v[1] : r == 2 ? v[2] : v[3];
+      to[row0 + 4 * qd + r] = ev == -128 ? -INFINITY : ev == kNotFinite ? INFINITY : v;
   }
 }
 
