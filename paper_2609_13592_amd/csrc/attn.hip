@@ -354,7 +354,9 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
 #endif
 // SEL: the blocks of the KV head's list in place of the whole context (the
 // list's partial block may stand anywhere, so tokens are counted per block).
-template <int G, bool WAVE, bool SEL>
+// ONE: no list has more than one partition: a workgroup for every (KV head,
+// request), empty ones too, which writes the output rows itself.
+template <int G, bool WAVE, bool SEL, bool ONE = false>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
     G == 8 || SEL ? 2 : BOOST_ATTN_WAVES))) void attn_partition(AttnParams P) {
   constexpr int kUnroll = G == 8 ? BOOST_ATTN_UNROLL8 : BOOST_ATTN_UNROLL;  // blocks in flight
@@ -370,14 +372,19 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   __shared__ int32_t s_tok[SEL ? kMaxPartBlocks : 1];  // tokens that count of each block
   __shared__ int s_red[4], s_pick[5];
   int part, b, g, L;
-  if constexpr (WAVE) {
+  if constexpr (ONE) {
+    b = blockIdx.x % P.B;
+    g = P.H - 1 - blockIdx.x / P.B;
+    part = 0;
+    L = P.lens[b];
+  } else if constexpr (WAVE) {
     if (!item_of_wave(P, blockIdx.x, b, g, part, L)) return;  // uniform
   } else {
     if (!item_of(P, blockIdx.x, b, g, part, L, s_red, row, s_pick)) return;  // uniform
   }
   const int n_blk = L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks);
   const int blk_beg = part * P.part_blocks;
-  if (blk_beg >= n_blk) return;  // uniform: empty partition (not produced by item_of)
+  if (!ONE && blk_beg >= n_blk) return;  // uniform: empty partition (not produced by item_of)
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
   // leading blocks whose 16 tokens are all inside the context
   const int nfull = SEL ? nbp : max(0, min(nbp, L / kT - blk_beg));
@@ -593,6 +600,25 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
       for (int e = 0; e < 8; ++e) a2[0][e] = s_acc[w][j][dc * 8 + e];
       merge_state<1>(&mj, &lj, aj, &m2, &l2, a2);
     }
+    if constexpr (ONE) {
+      const float inv = lj != 0.f ? 1.f / lj : 0.f;  // nothing counted: zeros
+      const int64_t oi = (static_cast<int64_t>(b) * P.Hq + g * G + j) * kD + dc * 8;
+      if (P.out_bf16) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          w[e] = to_bf16(aj[0][2 * e] * inv) |
+                 static_cast<uint32_t>(to_bf16(aj[0][2 * e + 1] * inv)) << 16;
+        uint32_t* const o = reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(P.out) + oi);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = w[e];
+      } else {
+        float* const o = static_cast<float*>(P.out) + oi;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = aj[0][e] * inv;
+      }
+      continue;
+    }
     const int64_t rowi = (static_cast<int64_t>(b) * P.Hq + g * G + j) * P.max_parts + part;
     if (dc == 0) {
       P.part_ml[rowi * 2] = mj;
@@ -750,6 +776,14 @@ template <int G, bool SEL>
 int launch_partitions(AttnParams& P, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
   if (grid > 0x7fffffff) return bst::fail(BOOST_EINVAL, "grid too large");
+  if constexpr (SEL) {
+    if (P.n_parts == 1) {
+      hipLaunchKernelGGL((attn_partition<G, true, true, true>), dim3(static_cast<unsigned>(grid)),
+                         dim3(kThreads), 0, s, P);
+      BOOST_HIP(hipGetLastError());
+      return BOOST_OK;
+    }
+  }
   // up to 64 requests the search by wavefronts, in a kernel of its own (64
   // requests of 512..4096 tokens, 32 / 8 heads: 106.7 us, 108.4 with the search
   // by barriers, 111.0 with both in one kernel, whose registers spill; one of
@@ -855,7 +889,14 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
       {kMaxPartBlocks, max_blocks,
        std::max(part_min, std::min(kPartMax, (max_blocks + want_parts - 1) / want_parts))});
   P.part_blocks = std::max(P.part_blocks, 4);
-  // a 4-bit context of one partition needs no merge
+  // a context or list of one partition needs no merge (attn4.hip has the
+  // 4-bit pools' figures). bf16 lists: short ones (8 blocks of 16 requests' 8 heads, the step with
+  // the index and the selection: 21.7 us against 24.8), and any up to 256 where
+  // the requests' heads fill the card one and a half times (384 heads: 47.1 us
+  // against 51.3 with 32 blocks, 95.0 against 103.2 with 100; 512 heads of 200
+  // blocks: 172 against 195). With 256 heads it is 57.2 against 54.5, 64 blocks.
+  if (!fp4 && sel && max_blocks <= (2 * B * H < 3 * ctx->n_cu ? 8 : 256))
+    P.part_blocks = std::max(max_blocks, 4);
   if (fp4 && max_blocks <= (B * H < ctx->n_cu / 2 ? kOneFew : kOneMany))
     P.part_blocks = std::max(max_blocks, 4);
   P.n_parts = (max_blocks + P.part_blocks - 1) / P.part_blocks;
@@ -876,7 +917,6 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   if (fp4) {
     if (G > 8) return fail(BOOST_EINVAL, "Hq/H=%d above 8", G);
     rc = launch_fp4(P, ctx->n_cu, s);
-    if (P.n_parts == 1) return rc;
   } else {
     switch (G) {
       case 1: rc = launch<1>(P, s); break;
@@ -886,7 +926,9 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
       default: return fail(BOOST_EINVAL, "Hq/H=%d not in {1, 2, 4, 8}", G);
     }
   }
-  return rc ? rc : launch_merge(P, sel || fp4, s);
+  // 4-bit pools and lists: contexts of one partition each are finished
+  if (rc || ((fp4 || sel) && P.n_parts == 1)) return rc;
+  return launch_merge(P, sel || fp4, s);
 }
 
 }  // namespace

@@ -22,9 +22,6 @@
 
 namespace {
 
-#ifndef BST_MID
-#define BST_MID 8192
-#endif
 constexpr int kD = 128;
 constexpr int kT = 16;
 constexpr int kSum = 2 * kD;      // bytes of a summary: hi, then -lo
@@ -665,11 +662,12 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   hipLaunchKernelGGL(block_scores_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, P,
                      chunks);
   BOOST_HIP(hipGetLastError());
-  // a workgroup as wide as the widest context has work for
+  // a workgroup as wide as the widest context has work for (8192 blocks, the
+  // step of one request: 33.9 us with 512 threads, 35.3 with 1024)
   const dim3 rows(static_cast<unsigned>(B) * H);
   if (max_blocks <= 2048)
     hipLaunchKernelGGL((select_blocks_kernel<256, 8>), rows, dim3(256), 0, s, P);
-  else if (max_blocks <= BST_MID)
+  else if (max_blocks <= 8192)
     hipLaunchKernelGGL((select_blocks_kernel<512, 16>), rows, dim3(512), 0, s, P);
   else
     hipLaunchKernelGGL((select_blocks_kernel<1024, 16>), rows, dim3(1024), 0, s, P);

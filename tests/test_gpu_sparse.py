@@ -156,6 +156,32 @@ def test_summaries_selection_and_attention(gpu_ctx, fmt, H, Hq):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("H,Hq", [(8, 32), (8, 8), (8, 64), (10, 20)])
+def test_whole_lists_of_many_heads(gpu_ctx, fmt, H, Hq):
+    """Enough heads to fill the card with a workgroup for each list: rows that
+    select nothing, requests without tokens, partial blocks anywhere."""
+    rng = np.random.default_rng(H + Hq)
+    lens = rng.integers(1, 700, size=50, endpoint=True)
+    lens[3] = lens[49] = 0
+    c = Cache(gpu_ctx, rng, fmt, lens, H, Hq)
+    try:
+        c.write()
+        n = (lens + 15) // 16
+        sel = np.full((50, H, 40), -1, np.int32)
+        for b in range(50):
+            for h in range(H):
+                m = min(40, int(n[b]))
+                sel[b, h, :m] = np.sort(rng.permutation(int(n[b]))[:m])
+        sel[7], sel[8, 1] = -1, -1
+        sel[9, 0, 1:] = -1
+        o = c.attend(sel)
+        c.check_attention(o, sel)
+        assert np.array_equal(c.attend(sel, bd.DTYPE_BF16), og.f32_to_bf16(o))
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_placement_does_not_change_a_bit(gpu_ctx, fmt):
     outs = []
     for mode, M in ((bd.KV_ALL_HBM, 0), (bd.KV_LPP, 2), (bd.KV_ALL_HOST, 0)):
