@@ -187,8 +187,12 @@ class DecodeModel:
 
     def bytes_per_step(self, lens) -> int:
         """Algorithmic bytes of one step: every weight matrix once, every
-        layer's K and V of every context token, plus the embedding rows."""
+        layer's K and V of every token attended to in the pool's format, with
+        top_blocks the summaries of every block, plus the embedding rows."""
         D = self.dims
         w = sum(N * K * 2 for _, N, K in D.shapes()) * D.layers + D.vocab * D.d * 2
-        kv = sum(int(L) for L in lens) * D.hkv * D.hd * 2 * 2 * D.layers
+        row = D.hd * 2 if bd.boost_kv_pool_format(self.pool) == bd.KV_BF16 else D.hd // 32 * 17
+        tokens = sum(min(int(L), 16 * self.top) if self.top else int(L) for L in lens)
+        blocks = sum((int(L) + 15) // 16 for L in lens) if self.top else 0
+        kv = (tokens * row * 2 + blocks * (2 * D.hd + 1)) * D.hkv * D.layers
         return w + kv + self.B * D.d * 2
