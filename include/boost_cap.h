@@ -469,8 +469,12 @@ int boost_kv_pool_create(boost_ctx *ctx, const boost_kv_cfg *cfg,
  * that takes a pool works on both: tokens are handed over and returned as
  * bf16, and attention over a 4-bit pool computes with the values that the
  * codes stand for (q exact, sums and softmax in fp32; probabilities enter the
- * product with V with 16 significant bits or more).  In a 4-bit pool blocks_per_page is 1920, and
- * attention takes any q_heads / kv_heads up to 8.
+ * product with V with 16 significant bits or more).  In a 4-bit pool
+ * blocks_per_page is 1920, attention takes any q_heads / kv_heads up to 8, and
+ * two tokens of one call must not go to the same slot (of bf16 rows either one
+ * is kept; codes and scales of both could mix).
+ * These calls, and on any pool boost_kv_read, boost_kv_copy_blocks and sparse
+ * attention's, are refused (EINVAL) while another device is the current one.
  * Errors: as boost_kv_pool_create; EINVAL (format, head_dim). */
 int boost_kv_pool_create_format(boost_ctx *ctx, const boost_kv_cfg *cfg, int format,
                                 boost_kv_pool **out);
@@ -522,7 +526,7 @@ int boost_kv_free(boost_kv_pool *pool, uint64_t request_id);
  * or more than the parent holds), ENOMEM.
  *
  * boost_kv_unshare: before the request writes into its index-th block.  Held by
- * it alone: *src = *dst = the block.  Shared: the request gets a free block
+ * it alone: *src = *dst = the block, and nothing to copy.  Shared: the request gets a free block
  * *dst in its place, as boost_kv_alloc hands one out, and the caller copies
  * *src to it.  Errors: EINVAL (unknown request, index), EAGAIN (no free block;
  * nothing changes).
@@ -638,7 +642,8 @@ int boost_paged_attn_decode_noalloc(boost_ctx *ctx, const boost_kv_pool *pool,
 
 /* Give the pool room for the summaries: 257 bytes of HBM per layer, KV head
  * and block, beside what tier_mode places (zero at first: score 0).  Freed
- * with the pool; again is a no-op.  Synchronises.  head_dim 128.
+ * with the pool; again is a no-op.  Synchronises (not inside graph capture).
+ * head_dim 128.
  * Errors: EINVAL, ENODEV, ENOMEM, EHIP. */
 int boost_kv_index_enable(boost_kv_pool *pool);
 
@@ -662,7 +667,8 @@ int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
  * like e), a block's score is
  *   max over the KV head's query heads of 2^(e + eq) sum_d max(q8 hi, q8 lo),
  * an upper bound of q8 . k; the sum is one of whole numbers, so scores are
- * exact and the selection is reproducible on every placement.  A query head
+ * exact (where fp32 holds them: +-inf from 2^128 on, rounded below 2^-126) and
+ * the selection is reproducible on every placement.  A query head
  * that is not finite counts as 0, a block outside the pool as -inf.
  * With n = ceil(ctx_lens[b] / T) blocks (at most max_blocks), the first
  * n_first and the last n_last of them are taken always, then those with the
@@ -671,7 +677,7 @@ int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
  * a request's blocks are left as they are.  sel: device int32 [B, H, top_k]:
  * indices of blocks in the context, ascending, then -1.
  * q: device bf16 [B, Hq, 128], 16-byte aligned, Hq / H up to 16.
- * n_first + n_last <= top_k.  Errors: EINVAL, ENODEV, EHIP. */
+ * n_first + n_last <= top_k <= 2^27.  Errors: EINVAL, ENODEV, EHIP. */
 int boost_kv_select(boost_ctx *ctx, const boost_kv_pool *pool, int layer, const void *q,
                     int B, int Hq, const int32_t *block_tables, int max_blocks,
                     const int32_t *ctx_lens, int top_k, int n_first, int n_last,
@@ -684,7 +690,7 @@ int boost_kv_select(boost_ctx *ctx, const boost_kv_pool *pool, int layer, const 
  * past it) is skipped, one that comes twice counts twice.  A list with every
  * block gives boost_paged_attn_decode's result up to rounding.
  * sel: device int32 [B, H, top_k].  Other arguments, scratch and errors as
- * boost_paged_attn_decode; EINVAL for top_k < 1. */
+ * boost_paged_attn_decode; EINVAL for top_k outside [1, 2^27]. */
 int boost_sparse_attn_decode(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
                              const void *q, int B, int Hq, const int32_t *block_tables,
                              int max_blocks, const int32_t *ctx_lens, const int32_t *sel,

@@ -382,7 +382,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   } else {
     if (!item_of(P, blockIdx.x, b, g, part, L, s_red, row, s_pick)) return;  // uniform
   }
-  const int n_blk = L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks);
+  const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
   const int blk_beg = part * P.part_blocks;
   if (!ONE && blk_beg >= n_blk) return;  // uniform: empty partition (not produced by item_of)
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
@@ -637,8 +637,8 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   const int b = bh / P.Hq;
   const int lane = threadIdx.x;
   const int L = P.lens[b];
-  const int n_blk = min((L + kT - 1) / kT, P.item_blocks);
-  const int np = L <= 0 ? 0 : (n_blk + P.part_blocks - 1) / P.part_blocks;
+  const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
+  const int np = (n_blk + P.part_blocks - 1) / P.part_blocks;
   const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
   // the largest partition maximum: one partition per lane, then across the
   // wavefront (a maximum is exact in any order)
@@ -698,8 +698,8 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
   const int bh = blockIdx.x, b = bh / P.Hq;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int L = P.lens[b];
-  const int n_blk = min((L + kT - 1) / kT, P.item_blocks);
-  const int np = L <= 0 ? 0 : (n_blk + P.part_blocks - 1) / P.part_blocks;
+  const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
+  const int np = (n_blk + P.part_blocks - 1) / P.part_blocks;
   if (np == 1 && P.one_done) return;  // uniform: the row is written
   const int per = (np + W - 1) / W, beg = min(np, wave * per), end = min(np, beg + per);
   const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
@@ -840,6 +840,8 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
   if (!ctx || !pool || !q || !block_tables || !ctx_lens || !out)
     return fail(BOOST_EINVAL, "null argument");
   if (ctx->device < 0 || !pool->d_page_table) return fail(BOOST_ENODEV, "plan-only pool");
+  if (sel || pool->format == BOOST_KV_FP4)
+    if (int rc = bst::kv_device(pool)) return rc;
   const boost_kv_cfg& c = pool->cfg;
   if (layer < 0 || static_cast<uint32_t>(layer) >= c.layers)
     return fail(BOOST_EINVAL, "layer %d", layer);
@@ -990,7 +992,7 @@ int boost_sparse_attn_decode(boost_ctx* ctx, const boost_kv_pool* pool, int laye
                              const int32_t* ctx_lens, const int32_t* sel, int top_k, float scale,
                              void* out, int out_dtype, void* stream) {
   if (!pool || !sel) return fail(BOOST_EINVAL, "null argument");
-  if (top_k < 1) return fail(BOOST_EINVAL, "top_k=%d", top_k);
+  if (top_k < 1 || top_k > bst::kMaxTop) return fail(BOOST_EINVAL, "top_k=%d", top_k);
   const int64_t rows = static_cast<int64_t>(pool->cfg.max_batch) * pool->cfg.q_heads *
                        std::max(1, pool->max_parts);
   return decode(ctx, pool, layer, q, B, Hq, block_tables, max_blocks, ctx_lens, scale, out,

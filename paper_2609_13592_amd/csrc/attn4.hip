@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int r = lane & 15, qd = lane >> 4;
   const int G = P.Hq / P.H;
-  const int n_blk = L <= 0 ? 0 : min((L - 1) / kT + 1, P.item_blocks);
+  const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
   const int blk_beg = part * P.part_blocks;
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
   const bool whole = n_blk <= P.part_blocks;

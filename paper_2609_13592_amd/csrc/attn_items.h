@@ -83,10 +83,13 @@ __device__ __forceinline__ uint16_t to_bf16(float f) {
   return static_cast<uint16_t>(u >> 16);
 }
 
+// Blocks of L > 0 tokens (any: L + 15 need not fit).
+__device__ __forceinline__ int blocks_in(int L) { return (L - 1) / kT + 1; }
+
 // Blocks of request b in this call (0 for an empty context).
 __device__ __forceinline__ int blocks_of(const AttnParams& P, int b) {
   const int L = P.lens[b];
-  return L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks);
+  return L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
 }
 
 // Sum of v over the workgroup; every thread gets it (red: 4 ints of LDS).
@@ -150,7 +153,7 @@ __device__ __forceinline__ bool item_of_wave(const AttnParams& P, int idx, int& 
                                              int& part, int& L) {
   const int lane = threadIdx.x & 63, PB = P.part_blocks, H = P.H;
   const int L0 = lane < P.B ? P.lens[lane] : 0;
-  const int n = L0 <= 0 ? 0 : min((L0 + kT - 1) / kT, P.item_blocks);
+  const int n = L0 <= 0 ? 0 : min(blocks_in(L0), P.item_blocks);
   const int full = n / PB, rem = n % PB;
   // inclusive prefix sums of both counts over the requests
   int xf = full, xr = rem > 0;
@@ -231,7 +234,7 @@ __device__ inline bool item_of(const AttnParams& P, int idx, int& b, int& g, int
   const int tid = threadIdx.x, PB = P.part_blocks, H = P.H;
   if (tid < 5) pick[tid] = -1;  // written by the sums' barriers below
   const int L0 = tid < P.B ? P.lens[tid] : 0;  // request tid, read once
-  const int n0 = L0 <= 0 ? 0 : min((L0 + kT - 1) / kT, P.item_blocks);
+  const int n0 = L0 <= 0 ? 0 : min(blocks_in(L0), P.item_blocks);
   int f = 0, r = 0;
   for (int bb = tid; bb < P.B; bb += kThreads) {
     const int n = bb == tid ? n0 : blocks_of(P, bb);
@@ -284,7 +287,7 @@ __device__ inline bool item_of(const AttnParams& P, int idx, int& b, int& g, int
   b = pick[0];
   if (b < 0 || b >= P.B) return false;
   L = pick[4];
-  part = (L <= 0 ? 0 : min((L + kT - 1) / kT, P.item_blocks)) / PB;
+  part = (L <= 0 ? 0 : min(blocks_in(L), P.item_blocks)) / PB;
   g = H - 2 - j % (H - 1);
   return true;
 }

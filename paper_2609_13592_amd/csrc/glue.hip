@@ -619,6 +619,8 @@ int boost_rope_kv_append_slices(boost_ctx* ctx, const boost_kv_pool* p, int laye
                     static_cast<int>(p->geom.nb)};
   // K = 0: no row of the producing matrix crosses a page
   const Slices sl{qkv, S, B, static_cast<int64_t>(Hq + 2 * H) * D, kPageElems % K ? K : 0};
+  if (p->format == BOOST_KV_FP4)
+    if (int rc = kv_device(p)) return rc;
   const auto kernel = p->format == BOOST_KV_FP4 ? rope_qkv_kernel<true, true>
                                                 : rope_qkv_kernel<true>;
   hipLaunchKernelGGL(kernel, dim3((B * (Hq + 2 * H) + kRopeWaves - 1) / kRopeWaves),

@@ -646,7 +646,7 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   if (B < 1 || max_blocks < 1) return fail(BOOST_EINVAL, "B=%d max_blocks=%d", B, max_blocks);
   if (Hq < H || Hq % H || Hq / H > 16)
     return fail(BOOST_EINVAL, "Hq=%d: a multiple of %d KV heads, up to 16 of each", Hq, H);
-  if (top_k < 1 || n_first < 0 || n_last < 0 ||
+  if (top_k < 1 || top_k > kMaxTop || n_first < 0 || n_last < 0 ||
       static_cast<int64_t>(n_first) + n_last > top_k)
     return fail(BOOST_EINVAL, "top_k=%d n_first=%d n_last=%d", top_k, n_first, n_last);
   if (reinterpret_cast<uintptr_t>(q) & 15) return fail(BOOST_EINVAL, "q must be 16-byte aligned");

@@ -4,6 +4,7 @@
 // one HBM slab; the device page table maps (layer, K/V, page) to an address.
 #include <algorithm>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <type_traits>
 
@@ -234,6 +235,8 @@ int guarded(F f) {
     return f();
   } catch (const std::bad_alloc&) {
     return bst::fail(BOOST_ENOMEM, "host memory for the allocator state");
+  } catch (const std::exception& e) {
+    return bst::fail(BOOST_EINVAL, "%s", e.what());
   }
 }
 
@@ -258,8 +261,18 @@ int kv_parts_for(const boost_kv_pool* p, int max_blocks) {
   return std::max(1, (tokens + kPartTokensMin - 1) / kPartTokensMin);
 }
 
-int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv) {
+int kv_device(const boost_kv_pool* p) {
   if (p->ctx->device < 0 || !p->d_page_table) return fail(BOOST_ENODEV, "plan-only pool");
+  int device = -1;
+  BOOST_HIP(hipGetDevice(&device));
+  if (device != p->ctx->device)
+    return fail(BOOST_EINVAL, "the pool is on device %d, the current one is %d", p->ctx->device,
+                device);
+  return BOOST_OK;
+}
+
+int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv) {
+  if (int rc = kv_device(p)) return rc;
   if (layer < 0 || static_cast<uint32_t>(layer) >= p->cfg.layers)
     return fail(BOOST_EINVAL, "layer %d", layer);
   *pk = p->d_page_table + (2ull * layer) * p->geom.pages;
@@ -535,7 +548,7 @@ int boost_kv_read(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int32
 int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int n_layers,
                          const int32_t* src, const int32_t* dst, int n, void* stream) {
   if (!ctx || !p || !src || !dst) return fail(BOOST_EINVAL, "null argument");
-  if (p->ctx->device < 0 || !p->d_page_table) return fail(BOOST_ENODEV, "plan-only pool");
+  if (int rc = kv_device(p)) return rc;
   if (layer0 < 0 || n_layers < 1 ||
       static_cast<int64_t>(layer0) + n_layers > static_cast<int64_t>(p->cfg.layers))
     return fail(BOOST_EINVAL, "layers [%d, %d + %d) of %u", layer0, layer0, n_layers,

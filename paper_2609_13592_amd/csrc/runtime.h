@@ -101,7 +101,13 @@ struct boost_kv_pool {
 
 namespace bst {
 
-// Page tables of one layer's K and V (ENODEV: plan-only pool, EINVAL: layer).
+// Longest list of blocks: as many as 2^31 tokens have.
+constexpr int kMaxTop = 1 << 27;
+
+// ENODEV: plan-only pool; EINVAL: its device is not the current one.
+int kv_device(const boost_kv_pool* p);
+
+// Page tables of one layer's K and V (as kv_device, and EINVAL: layer).
 int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv);
 
 // n rows [H, 128] of K and V into a 4-bit pool, at the given slots or (slots

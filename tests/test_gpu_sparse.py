@@ -182,6 +182,34 @@ def test_whole_lists_of_many_heads(gpu_ctx, fmt, H, Hq):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B", [3, 70])
+def test_lengths_past_the_table(gpu_ctx, fmt, B):
+    """Contexts as long as an int32 goes end with the table, in every call."""
+    rng = np.random.default_rng(B)
+    c = Cache(gpu_ctx, rng, fmt, [480] * B, 2, 8)
+    try:
+        c.write()
+        bd.boost_kv_index_enable(c.pool)
+        c.index()
+        sel = c.check_selection(12, 1, 1)
+
+        def dense():
+            o = dev_f32(B, 8, 128)
+            bd.boost_paged_attn_decode(gpu_ctx, c.pool, 0, to_dev_u16(c.q), B, 8, dev_i32(c.tables), c.mb,
+                                       dev_i32(c.lens), 0.0, o, bd.DTYPE_F32, stream())
+            sync()
+            return o.cpu().numpy()
+        want = (c.attend(sel), dense())
+        c.lens = np.array([2 ** 31 - 1 - i % 20 for i in range(B)])
+        c.index(hint=480)
+        assert np.array_equal(c.select(12, 1, 1)[1], sel)
+        for a, b in zip((c.attend(sel), dense()), want):
+            assert np.array_equal(a, b)
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_placement_does_not_change_a_bit(gpu_ctx, fmt):
     outs = []
     for mode, M in ((bd.KV_ALL_HBM, 0), (bd.KV_LPP, 2), (bd.KV_ALL_HOST, 0)):
@@ -441,6 +469,24 @@ def test_refusals(gpu_ctx):
         sync()
         bd.boost_kv_pool_destroy(pool)
         bd.boost_kv_pool_destroy(small)
+
+
+def test_lists_too_long(gpu_ctx):
+    import torch
+    pool = bd.boost_kv_pool_create(gpu_ctx, 1, 2, 128, 100, 0, bd.KV_ALL_HBM, q_heads=8, max_batch=1,
+                                   max_blocks_per_seq=8)
+    try:
+        bd.boost_kv_index_enable(pool)
+        z = torch.zeros(8 * 128, dtype=torch.int32, device="cuda")
+        for top in (2 ** 27 + 1, 2 ** 31 - 1):
+            for f in (lambda: bd.boost_kv_select(gpu_ctx, pool, 0, z, 1, 8, z, 8, z, top, 0, 0, z, z, stream()),
+                      lambda: bd.boost_sparse_attn_decode(gpu_ctx, pool, 0, z, 1, 8, z, 8, z, z, top, 0.0, z,
+                                                          bd.DTYPE_F32, stream())):
+                with pytest.raises(bd.BoostError) as e:
+                    f()
+                assert e.value.code == bd.EINVAL
+    finally:
+        bd.boost_kv_pool_destroy(pool)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
