@@ -178,9 +178,13 @@ __global__ __launch_bounds__(16 * kRows4) void kv_read4_kernel(
 // Blocks copied within the pool: one workgroup per (pair, KV head of K or V,
 // layer), and per (pair, KV head's summary, layer) where the pool has
 // summaries.  Read once and written once: bound by the bytes.
-constexpr int kCopyPairs = 448;  // per launch: the pairs travel as an argument
+// Pairs per launch: they travel as an argument, whose every byte the host
+// writes at each launch (a call for one pair: 4.0 us with room for 16, 4.5 with
+// room for 448).
+constexpr int kCopyFew = 16, kCopyPairs = 448;
+template <int N>
 struct CopyPairs {
-  int32_t src[kCopyPairs], dst[kCopyPairs];
+  int32_t src[N], dst[N];
 };
 struct CopyParams {
   const char* const* table;  // the pool's pages [layers][2][pages]
@@ -191,8 +195,8 @@ struct CopyParams {
   uint32_t block_bytes;      // bf16: bytes of a head-block
 };
 
-template <bool FP4>
-__global__ __launch_bounds__(256) void copy_blocks_kernel(CopyParams P, CopyPairs pairs) {
+template <bool FP4, int N>
+__global__ __launch_bounds__(256) void copy_blocks_kernel(CopyParams P, CopyPairs<N> pairs) {
   using namespace bst;
   const int tid = threadIdx.x;
   const int s = pairs.src[blockIdx.x], d = pairs.dst[blockIdx.x];
@@ -576,18 +580,23 @@ int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int
   const CopyParams P{p->d_page_table, p->geom.pages, p->d_index,
                      static_cast<uint64_t>(p->cfg.layers) * H * nb, layer0, H, nb,
                      p->cfg.block_tokens * p->cfg.head_dim * 2};
-  const auto kernel = p->format == BOOST_KV_FP4 ? copy_blocks_kernel<true>
-                                                : copy_blocks_kernel<false>;
-  for (int i = 0; i < n; i += kCopyPairs) {
-    CopyPairs pairs;
-    const int m = std::min(n - i, kCopyPairs);
-    std::copy_n(src + i, m, pairs.src);
-    std::copy_n(dst + i, m, pairs.dst);
-    hipLaunchKernelGGL(kernel, dim3(m, H * tensors, n_layers), dim3(256), 0,
-                       static_cast<hipStream_t>(stream), P, pairs);
-    BOOST_HIP(hipGetLastError());
-  }
-  return BOOST_OK;
+  auto launch = [&](auto per_launch) {
+    constexpr int N = decltype(per_launch)::value;
+    const auto kernel = p->format == BOOST_KV_FP4 ? copy_blocks_kernel<true, N>
+                                                  : copy_blocks_kernel<false, N>;
+    for (int i = 0; i < n; i += N) {
+      CopyPairs<N> pairs;
+      const int m = std::min(n - i, N);
+      std::copy_n(src + i, m, pairs.src);
+      std::copy_n(dst + i, m, pairs.dst);
+      hipLaunchKernelGGL(kernel, dim3(m, H * tensors, n_layers), dim3(256), 0,
+                         static_cast<hipStream_t>(stream), P, pairs);
+      BOOST_HIP(hipGetLastError());
+    }
+    return BOOST_OK;
+  };
+  return n <= kCopyFew ? launch(std::integral_constant<int, kCopyFew>{})
+                       : launch(std::integral_constant<int, kCopyPairs>{});
 }
 
 }  // extern "C"
