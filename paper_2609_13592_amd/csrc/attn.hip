@@ -891,14 +891,18 @@ int decode(boost_ctx* ctx, const boost_kv_pool* pool, int layer, const void* q, 
       {kMaxPartBlocks, max_blocks,
        std::max(part_min, std::min(kPartMax, (max_blocks + want_parts - 1) / want_parts))});
   P.part_blocks = std::max(P.part_blocks, 4);
-  // a context or list of one partition needs no merge (attn4.hip has the
-  // 4-bit pools' figures). bf16 lists: short ones (8 blocks of 16 requests' 8 heads, the step with
-  // the index and the selection: 21.7 us against 24.8), and any up to 256 where
-  // the requests' heads fill the card one and a half times (384 heads: 47.1 us
-  // against 51.3 with 32 blocks, 95.0 against 103.2 with 100; 512 heads of 200
-  // blocks: 172 against 195). With 256 heads it is 57.2 against 54.5, 64 blocks.
-  if (!fp4 && sel && max_blocks <= (2 * B * H < 3 * ctx->n_cu ? 8 : 256))
-    P.part_blocks = std::max(max_blocks, 4);
+  // Lists of a bf16 pool: as many partitions as fill the card once at two
+  // workgroups a compute unit (steps with the index and the selection, against
+  // partitions of 16 blocks: 16 requests with 8 KV heads, 32 blocks 32.9 -> 30.3
+  // us, 100 blocks 52.0 -> 45.6; 32 requests, 64 blocks 54.3 -> 49.0; whole
+  // lists at 384 heads, 32 blocks 51.3 -> 47.1, at 512, 64 blocks 90.0 -> 71.3).
+  // One of up to 8 blocks is not worth a merge (16 requests: 24.8 -> 21.7).
+  if (!fp4 && sel) {
+    const int parts = std::max(1, 2 * ctx->n_cu / (B * H));
+    P.part_blocks = std::min(kMaxPartBlocks, std::max(max_blocks <= 8 ? 8 : 4,
+                                                      (max_blocks + parts - 1) / parts));
+  }
+  // a 4-bit context or list of one partition needs no merge
   if (fp4 && max_blocks <= (B * H < ctx->n_cu / 2 ? kOneFew : kOneMany))
     P.part_blocks = std::max(max_blocks, 4);
   P.n_parts = (max_blocks + P.part_blocks - 1) / P.part_blocks;

@@ -662,11 +662,12 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   hipLaunchKernelGGL(block_scores_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, P,
                      chunks);
   BOOST_HIP(hipGetLastError());
-  // a workgroup as wide as the widest context has work for (8192 blocks, the
-  // step of one request: 33.9 us with 512 threads, 35.3 with 1024)
+  // keys in registers as far as they go (a step of 16 requests of up to 1875
+  // blocks 46.2 us with 512 threads, 47.5 with 256, 46.5 with 1024; of one with
+  // 8192 blocks 33.9 with 512, 35.3 with 1024)
   const dim3 rows(static_cast<unsigned>(B) * H);
   if (max_blocks <= 2048)
-    hipLaunchKernelGGL((select_blocks_kernel<256, 8>), rows, dim3(256), 0, s, P);
+    hipLaunchKernelGGL((select_blocks_kernel<512, 4>), rows, dim3(512), 0, s, P);
   else if (max_blocks <= 8192)
     hipLaunchKernelGGL((select_blocks_kernel<512, 16>), rows, dim3(512), 0, s, P);
   else
