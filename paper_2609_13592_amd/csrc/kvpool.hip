@@ -65,6 +65,19 @@ __global__ __launch_bounds__(256) void kv_read_kernel(
 // head-block's lines put together in one L2.
 constexpr int kRows4 = 16;
 
+// 16 bytes that are read or written once, past the caches, where the pool's
+// lines wait to be whole (write and read back of 20011 tokens with 8 heads, 207
+// MB: 45.5 us through them, 38.4 with the reads past them, 37.6 with the writes;
+// of 2000 7.5 and 6.8 with the writes, of 100000 214 and 174).
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+__device__ __forceinline__ uint4 streamed(const uint4* at) {
+  const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at));
+  return make_uint4(x[0], x[1], x[2], x[3]);
+}
+__device__ __forceinline__ void streamed(uint4* at, const uint4& v) {
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(at));
+}
+
 // Slot of row i: given (slots), or that of request i's token at pos[i] (a
 // position or a block outside the table or the pool: -1).
 struct RowSlot {
@@ -145,7 +158,7 @@ __global__ __launch_bounds__(16 * kRows4) void kv_write4_kernel(
   const int64_t slot = slot_of(rows, i, nb);
   if (slot < 0) return;
   const int64_t at = (i * H + h) * 16 + r;
-  const uint4 uk = k[at], uv = v[at];
+  const uint4 uk = streamed(k + at), uv = streamed(v + at);
   const Row4 to = row4(pt_k, pt_v, slot, h, nb, r);
   uint32_t sk, sv;
   const uint32_t ck = codes_of(uk, sk), cv = codes_of(uv, sv);
@@ -171,13 +184,17 @@ __global__ __launch_bounds__(16 * kRows4) void kv_read4_kernel(
   const uint32_t ck = *reinterpret_cast<const uint32_t*>(from.k);
   const uint32_t cv = *reinterpret_cast<const uint32_t*>(from.v);
   const uint32_t sk = static_cast<uint8_t>(*from.ks), sv = static_cast<uint8_t>(*from.vs);
-  k[at] = values_of(ck, sk);
-  v[at] = values_of(cv, sv);
+  streamed(k + at, values_of(ck, sk));
+  streamed(v + at, values_of(cv, sv));
 }
 
-// Blocks copied within the pool: one workgroup per (pair, KV head of K or V,
-// layer), and per (pair, KV head's summary, layer) where the pool has
-// summaries.  Read once and written once: bound by the bytes.
+// Blocks copied within the pool: one workgroup (4 bits: wavefront) per (pair,
+// KV head of K or V, layer), and per (pair, KV head's summary, layer) where the
+// pool has summaries.  Read once and written once, past the caches: bound by
+// the bytes (61 blocks of 8 heads in 32 layers, bf16 44.5 us, 5.7 TB/s;
+// through the caches 52.0, with reads past them too 49.0; 200 blocks 119, 134
+// and 144.  4 bits: 61 blocks 15.4 us, by workgroups 19.2, through the caches
+// 21.3).
 // Pairs per launch: they travel as an argument, whose every byte the host
 // writes at each launch (a call for one pair: 4.0 us with room for 16, 4.5 with
 // room for 448).
@@ -192,15 +209,18 @@ struct CopyParams {
   int8_t* index;             // summaries and exponents, or null
   uint64_t index_blocks;     // layers * H * nb
   int layer0, H, nb;
+  int units;                 // KV heads of K, of V and of the summaries
   uint32_t block_bytes;      // bf16: bytes of a head-block
 };
 
 template <bool FP4, int N>
 __global__ __launch_bounds__(256) void copy_blocks_kernel(CopyParams P, CopyPairs<N> pairs) {
   using namespace bst;
-  const int tid = threadIdx.x;
   const int s = pairs.src[blockIdx.x], d = pairs.dst[blockIdx.x];
-  const int which = blockIdx.y / P.H, h = blockIdx.y % P.H;
+  const int tid = FP4 ? threadIdx.x & 63 : threadIdx.x;
+  const int unit = FP4 ? blockIdx.y * 4 + (threadIdx.x >> 6) : blockIdx.y;
+  if (FP4 && unit >= P.units) return;
+  const int which = unit / P.H, h = unit % P.H;
   const int layer = P.layer0 + static_cast<int>(blockIdx.z);
   if (which == 2) {
     const int64_t at = (static_cast<int64_t>(layer) * P.H + h) * P.nb;
@@ -215,20 +235,20 @@ __global__ __launch_bounds__(256) void copy_blocks_kernel(CopyParams P, CopyPair
     const Fp4At a = fp4_at(h, s, P.nb), b = fp4_at(h, d, P.nb);
     const char* const from = pt[a.page];
     char* const to = const_cast<char*>(pt[b.page]);
+    auto copy = [&](uint32_t dst, uint32_t src) {
+      streamed(reinterpret_cast<uint4*>(to + dst), *reinterpret_cast<const uint4*>(from + src));
+    };
     const uint32_t off = static_cast<uint32_t>(tid) * 16;
-    if (off < kFp4Code)
-      *reinterpret_cast<uint4*>(to + b.idx * kFp4Code + off) =
-          *reinterpret_cast<const uint4*>(from + a.idx * kFp4Code + off);
-    else if (off < kFp4Code + kFp4Scale)
-      *reinterpret_cast<uint4*>(to + kFp4ScaleAt + b.idx * kFp4Scale + off - kFp4Code) =
-          *reinterpret_cast<const uint4*>(from + kFp4ScaleAt + a.idx * kFp4Scale + off - kFp4Code);
+    copy(b.idx * kFp4Code + off, a.idx * kFp4Code + off);
+    if (off < kFp4Scale)
+      copy(kFp4ScaleAt + b.idx * kFp4Scale + off, kFp4ScaleAt + a.idx * kFp4Scale + off);
   } else {
     const uint64_t a = (static_cast<uint64_t>(h) * P.nb + s) * P.block_bytes;
     const uint64_t b = (static_cast<uint64_t>(h) * P.nb + d) * P.block_bytes;
     const uint32_t off = static_cast<uint32_t>(tid) * 16;
     if (off < P.block_bytes)
-      *reinterpret_cast<uint4*>(const_cast<char*>(pt[b >> 21]) + (b & (kPage - 1)) + off) =
-          *reinterpret_cast<const uint4*>(pt[a >> 21] + (a & (kPage - 1)) + off);
+      streamed(reinterpret_cast<uint4*>(const_cast<char*>(pt[b >> 21]) + (b & (kPage - 1)) + off),
+               *reinterpret_cast<const uint4*>(pt[a >> 21] + (a & (kPage - 1)) + off));
   }
 }
 
@@ -579,7 +599,8 @@ int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int
   if (rc) return rc;
   const CopyParams P{p->d_page_table, p->geom.pages, p->d_index,
                      static_cast<uint64_t>(p->cfg.layers) * H * nb, layer0, H, nb,
-                     p->cfg.block_tokens * p->cfg.head_dim * 2};
+                     H * tensors, p->cfg.block_tokens * p->cfg.head_dim * 2};
+  const int rows = p->format == BOOST_KV_FP4 ? (H * tensors + 3) / 4 : H * tensors;
   auto launch = [&](auto per_launch) {
     constexpr int N = decltype(per_launch)::value;
     const auto kernel = p->format == BOOST_KV_FP4 ? copy_blocks_kernel<true, N>
@@ -589,7 +610,7 @@ int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int
       const int m = std::min(n - i, N);
       std::copy_n(src + i, m, pairs.src);
       std::copy_n(dst + i, m, pairs.dst);
-      hipLaunchKernelGGL(kernel, dim3(m, H * tensors, n_layers), dim3(256), 0,
+      hipLaunchKernelGGL(kernel, dim3(m, rows, n_layers), dim3(256), 0,
                          static_cast<hipStream_t>(stream), P, pairs);
       BOOST_HIP(hipGetLastError());
     }
