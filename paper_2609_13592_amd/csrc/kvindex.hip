@@ -379,18 +379,34 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
   }
 }
 
+// Sum of v over this lane and those before it.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);  // the lane before, in its row of 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);  // 2 before
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);  // 4
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);  // 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);  // row 0 to 1, 2 to 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);  // rows 0 and 1 to 2 and 3
+  return v;
+}
+
 // One workgroup per (request, KV head): the top_k-th largest key by its
 // digits, then the keys above it and the first of those equal to it, in order.
 // Thread t holds keys t, NT + t, ..., V of them in registers (those past
 // V * NT blocks are read again in every pass).  The digits start at the
 // highest bit in which any two keys differ (scores of one query differ little
 // in their exponents: from bit 31 on, most keys would meet in one counter) and
-// end when no key is left to decide.  Bound by its passes' barriers, not by
-// the 4 bytes a block.
+// end when no key is left to decide.  Bound by the instructions of its few
+// wavefronts between its barriers, not by the 4 bytes a block: nothing
+// branches on a key, a digit is one barrier (every wavefront sums the counters
+// for itself) and has counters of its own, four of each so that equal digits
+// do not all wait for one another.
 template <int NT, int V>
 __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   constexpr int kWaves = NT / 64, kRound = 64;  // chunks of NT keys ranked at a time
-  __shared__ int hist[256], s_pick[3];
+  constexpr int kCopies = 4, kDigits = 4, kCounters = 256 * kCopies;
+  // of each digit, and 64 that nothing reads, for keys that do not count
+  __shared__ __align__(16) int hist[kDigits * kCounters + 64];
   __shared__ int s_cnt[kRound * (kWaves + 1)];  // above | equal << 16, of a chunk's wavefronts
   __shared__ uint32_t s_bits[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -415,25 +431,23 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   float own[V];  // loaded without a branch, all of them together
 #pragma unroll
   for (int j = 0; j < V; ++j) own[j] = scores[min(j * NT + tid, n - 1)];
+  for (int i = tid; i < kDigits * kCounters / 4; i += NT)
+    reinterpret_cast<i32x4*>(hist)[i] = i32x4{0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const uint32_t k = key_of(own[j], j * NT + tid);
     key[j] = j * NT + tid < n ? k : kAlways;
   }
-  auto each = [&](auto f) {  // the keys that are to be ordered
+  auto each = [&](auto f) {  // kAlways among them
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (key[j] != kAlways) f(key[j]);
-    for (int i = V * NT + tid; i < n; i += NT) {
-      const uint32_t k = key_at(i);
-      if (k != kAlways) f(k);
-    }
+    for (int j = 0; j < V; ++j) f(key[j]);
+    for (int i = V * NT + tid; i < n; i += NT) f(key_at(i));
   };
   // bits in which keys differ: set in one and clear in another
   uint32_t any1 = 0, any0 = 0;
   each([&](uint32_t k) {
-    any1 |= k;
-    any0 |= ~k;
+    any1 |= k == kAlways ? 0u : k;
+    any0 |= ~k;  // (of kAlways: none)
   });
   auto either = [](uint32_t x, uint32_t y) { return x | y; };
   auto over_wave = [&](uint32_t v) {
@@ -449,7 +463,6 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
     s_bits[0][wave] = any1;
     s_bits[1][wave] = any0;
   }
-  for (int i = tid; i < 256; i += NT) hist[i] = 0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
@@ -464,51 +477,37 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   // the last blocks are apart)
   int need = P.top_k - P.n_first - P.n_last;
   bool open = need > 0;
-  while (open && top > 0) {
+  for (int* h = hist; open && top > 0; h += kCounters) {  // at most four digits
     const int shift = max(0, top - 8);
-    const uint32_t digit = (1u << (top - shift)) - 1;
+    const uint32_t digit = (1u << (top - shift)) - 1, decided = top == 32 ? 0u : ~0u << top;
+    const uint32_t mine = lane % kCopies;
+    const uint32_t out = static_cast<uint32_t>(hist + kDigits * kCounters - h) + lane;
     each([&](uint32_t k) {
-      if (top == 32 || (k ^ least) >> top == 0) {
-        // one addition for a wavefront whose keys agree (equal scores)
-        const uint32_t d = (k >> shift) & digit;
-        const unsigned long long here = __ballot(1);
-        if (__ballot(d == static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(d))) == here) {
-          if (lane == __ffsll(here) - 1) atomicAdd(&hist[d], static_cast<int>(__popcll(here)));
-        } else {
-          atomicAdd(&hist[d], 1);
-        }
-      }
+      const uint32_t d = (k >> shift & digit) * kCopies + mine;
+      atomicAdd(&h[((k ^ least) & decided) == 0 && k != kAlways ? d : out], 1);
     });
     __syncthreads();
-    if (wave == 0) {  // lane l: digits 255 - 4 l, ... - 3, with the keys above them
-      int c[4], x = 0;
+    // lane l: digits 255 - 4 l, ... - 3, with the keys above them
+    int c[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c[j] = hist[255 - 4 * lane - j];
-        hist[255 - 4 * lane - j] = 0;  // for the next digit
-        x += c[j];
-      }
-      int before = x;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const int y = __shfl_up(before, d, 64);
-        if (lane >= d) before += y;
-      }
-      before -= x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (before < need && before + c[j] >= need) {
-          s_pick[0] = 255 - 4 * lane - j;
-          s_pick[1] = need - before;
-          s_pick[2] = c[j];
-        }
-        before += c[j];
-      }
+    for (int j = 0; j < 4; ++j) {
+      const i32x4 u = *reinterpret_cast<const i32x4*>(&h[(255 - 4 * lane - j) * kCopies]);
+      c[j] = u[0] + u[1] + u[2] + u[3];
     }
-    __syncthreads();
-    least |= static_cast<uint32_t>(s_pick[0]) << shift;
-    need = s_pick[1];
-    open = s_pick[2] != need;  // else every key of this digit is taken
+    const int x = c[0] + c[1] + c[2] + c[3], upto = wave_scan(x);
+    int before = upto - x, pick = 0, take = 0, count = 0;
+    const int l = __ffsll(__ballot(before < need && upto >= need)) - 1;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const bool here = before < need && before + c[j] >= need;
+      pick = here ? 255 - 4 * lane - j : pick;
+      take = here ? need - before : take;
+      count = here ? c[j] : count;
+      before += c[j];
+    }
+    least |= static_cast<uint32_t>(__builtin_amdgcn_readlane(pick, l)) << shift;
+    need = __builtin_amdgcn_readlane(take, l);
+    open = __builtin_amdgcn_readlane(count, l) != need;  // else every key of this digit is taken
     top = shift;
   }
   // keys above `upto` are taken, and the first `need` from least to there
@@ -519,12 +518,12 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   for (int c0 = 0; c0 < chunks; c0 += kRound) {
     const int m = min(kRound, chunks - c0);
     // lane j: this wavefront's 64 blocks of chunk j that are above, and equal
-    unsigned long long gt = 0, eq = 0;
+    unsigned long long gt_own = 0, eq_own = 0;
     auto mark = [&](int j, uint32_t k, bool in) {  // all lanes together
       const bool more = in && (k > upto || k == kAlways);
       const unsigned long long x = __ballot(more), y = __ballot(in && !more && k >= least);
-      gt = lane == j ? x : gt;
-      eq = lane == j ? y : eq;
+      gt_own = lane == j ? x : gt_own;
+      eq_own = lane == j ? y : eq_own;
     };
     if (c0 == 0) {
 #pragma unroll
@@ -535,7 +534,7 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
       mark(j, key_at(min(i, n - 1)), i < n);
     }
     if (c0 > 0) __syncthreads();  // s_cnt is free again
-    s_cnt[lane * (kWaves + 1) + wave] = __popcll(gt) | __popcll(eq) << 16;
+    s_cnt[lane * (kWaves + 1) + wave] = __popcll(gt_own) | __popcll(eq_own) << 16;
     __syncthreads();
     // what stands before: in the chunk, then in the chunks before it
     int x = 0, y = 0, own_x = 0, own_y = 0;
@@ -547,32 +546,28 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
       x += c & 0xffff;
       y += c >> 16;
     }
-    int sx = x, sy = y;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int u = __shfl_up(sx, d, 64), v = __shfl_up(sy, d, 64);
-      if (lane >= d) {
-        sx += u;
-        sy += v;
-      }
-    }
+    const int sx = wave_scan(x), sy = wave_scan(y);
     own_x += above0 + sx - x;
     own_y += equal0 + sy - y;
     above0 += __builtin_amdgcn_readlane(sx, 63);
     equal0 += __builtin_amdgcn_readlane(sy, 63);
-    // the words of which something is taken, one by one, a lane a block
-    const unsigned long long below = (1ull << lane) - 1;
-    for (unsigned long long words = __ballot(gt || (eq && own_y < need)); words; words &= words - 1) {
-      const int j = __ffsll(words) - 1;
-      auto lane_of = [&](unsigned long long v) {
-        return static_cast<unsigned long long>(__builtin_amdgcn_readlane(static_cast<int>(v >> 32), j)) << 32 |
-               static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), j));
-      };
-      const unsigned long long g = lane_of(gt), q = lane_of(eq);
-      const int a = __builtin_amdgcn_readlane(own_x, j) + static_cast<int>(__popcll(g & below));
-      const int e = __builtin_amdgcn_readlane(own_y, j) + static_cast<int>(__popcll(q & below));
-      if ((g >> lane & 1) || ((q >> lane & 1) && e < need))
-        sel[a + min(e, need)] = (c0 + j) * NT + tid;
+    // the words again by all lanes: of a round of up to 4, 16 or 64 chunks a
+    // lane has so many bits of one word, and writes those that are taken
+    const int lg = m <= 4 ? 2 : m <= 16 ? 4 : 6;
+    const int j = lane >> (6 - lg), from = (lane & ((64 >> lg) - 1)) << lg;
+    unsigned long long gt = __shfl(gt_own, j, 64), eq = __shfl(eq_own, j, 64);
+    const unsigned long long below = (1ull << from) - 1, bits = ~0ull >> (64 - (1 << lg));
+    int a = __shfl(own_x, j, 64) + static_cast<int>(__popcll(gt & below));
+    int e = __shfl(own_y, j, 64) + static_cast<int>(__popcll(eq & below));
+    gt = gt >> from & bits;
+    eq = e < need ? eq >> from & bits : 0;
+    const int i0 = (c0 + j) * NT + 64 * wave + from;
+    for (unsigned long long left = gt | eq; left; left &= left - 1) {
+      const int i = __ffsll(left) - 1;
+      const bool above = gt >> i & 1;
+      if (above || e < need) sel[a + min(e, need)] = i0 + i;
+      a += above;
+      e += !above;
     }
   }
 }
@@ -662,16 +657,20 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   hipLaunchKernelGGL(block_scores_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, P,
                      chunks);
   BOOST_HIP(hipGetLastError());
-  // keys in registers as far as they go (a step of 16 requests of up to 1875
-  // blocks 46.2 us with 512 threads, 47.5 with 256, 46.5 with 1024; of one with
-  // 8192 blocks 33.9 with 512, 35.3 with 1024)
+  // keys in registers as far as they go, and no more wavefronts than have work
+  // (whole steps: 64 requests of 250 blocks 46.5 us with 256 threads, 48.4 with
+  // 512; 16 of up to 1875 blocks 44.8 with 512, 46.2 with 1024; one of 8192 28.1
+  // with 512, 28.8 with 1024 and 30.6 with 256; one of 31250 45.5 with 32 keys a
+  // thread, 54.5 with 16 and the rest read again in every pass)
   const dim3 rows(static_cast<unsigned>(B) * H);
-  if (max_blocks <= 2048)
+  if (max_blocks <= 512)
+    hipLaunchKernelGGL((select_blocks_kernel<256, 2>), rows, dim3(256), 0, s, P);
+  else if (max_blocks <= 2048)
     hipLaunchKernelGGL((select_blocks_kernel<512, 4>), rows, dim3(512), 0, s, P);
   else if (max_blocks <= 8192)
     hipLaunchKernelGGL((select_blocks_kernel<512, 16>), rows, dim3(512), 0, s, P);
   else
-    hipLaunchKernelGGL((select_blocks_kernel<1024, 16>), rows, dim3(1024), 0, s, P);
+    hipLaunchKernelGGL((select_blocks_kernel<1024, 32>), rows, dim3(1024), 0, s, P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

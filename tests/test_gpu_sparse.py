@@ -249,6 +249,37 @@ def test_sizes(gpu_ctx, fmt, B, hi):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n", [512, 2048, 8193, 32769, 70001])
+def test_selection_over_tables_of_every_width(gpu_ctx, fmt, n):
+    """Tables that name each of 300 blocks (and some that are none) many times:
+    many equal scores, and every way a workgroup holds the keys."""
+    import torch
+    rng = np.random.default_rng(n)
+    H, Hq = 2, 8
+    c = Cache(gpu_ctx, rng, fmt, [4800], H, Hq)
+    try:
+        c.write()
+        bd.boost_kv_index_enable(c.pool)
+        c.index()
+        one = osel.scores(og.bf16_to_f32(c.q[0]).astype(np.float64), c.meaning(c.k[0]))  # [H, 300]
+        at = rng.integers(0, 300, size=n)
+        table = c.tables[0, at][None].copy()
+        want = one[:, at]
+        none = rng.random(n) < 0.01
+        table[0, none], want[:, none] = -1, -np.inf
+        for top, first, last in ((1, 0, 0), (5, 2, 3), (300, 1, 2), (n // 2, 0, 1), (n - 1, 1, 0)):
+            sc = torch.full((1, H, n), 77.0, dtype=torch.float32, device="cuda")
+            sel = torch.full((1, H, top), 99, dtype=torch.int32, device="cuda")
+            bd.boost_kv_select(gpu_ctx, c.pool, 0, to_dev_u16(c.q), 1, Hq, dev_i32(table), n,
+                               dev_i32([16 * n - 5]), top, first, last, sc, sel, stream())
+            sync()
+            assert np.array_equal(sc.cpu().numpy()[0], want)
+            assert np.array_equal(sel.cpu().numpy()[0], osel.select(want, top, first, last)), top
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 def test_updates_block_by_block(gpu_ctx, fmt):
     """A context that grows: updates of one token, of a few, of ranges that
     the hint is too small for, leave the same summaries as one over all; other
