@@ -255,12 +255,13 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
   return L <= 0 ? 0 : min((L - 1) / kT + 1, P.max_blocks);
 }
 
-// Scores of 16-block tiles, four to a wavefront: rows are blocks, columns the
-// KV head's query heads, the 256 products of a pair in four 16x16x64 integer
+// Scores of 16-block tiles, four to a wavefront: rows are the KV head's query
+// heads, columns blocks, the 256 products of a pair in four 16x16x64 integer
 // products (hi against the positive part of q8, -lo against the magnitude of
-// the negative one).  Bound by the summaries' bytes and the chain before them
-// (lengths, block ids): the loads of all four tiles are out together, and q is
-// rounded while they are, a quarter by each wavefront.
+// the negative one), so that a lane ends with four heads of one block.  Bound by
+// the summaries' bytes and the chain before them (block ids): the loads of all
+// four tiles are out together, and q is rounded while they are, a quarter by
+// each wavefront.
 constexpr int kTileBlocks = 16, kTiles = 4;
 constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
@@ -271,8 +272,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
   const int chunk = blockIdx.x % chunks, bg = blockIdx.x / chunks;
   const int g = bg % P.H, b = bg / P.H;
-  const int n = context_blocks(P, b);
-  if (chunk * kScoreBlocks >= n) return;  // uniform
+  const int L = P.lens[b];  // (the ids do not wait for it)
   const int first = chunk * kScoreBlocks + wave * kTiles * kTileBlocks;
   const int G = P.Hq / P.H;
   const int8_t* const sum = P.sum + static_cast<int64_t>(g) * P.nb * kSum;
@@ -280,11 +280,11 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
   const int32_t* const table = P.tables + static_cast<int64_t>(b) * P.max_blocks;
   int32_t id[kTiles];
   i32x4 a[kTiles][4];
-  int e[kTiles];  // of block (row) r; -128: no such block
+  int e[kTiles];  // of block (column) r; -128: no such block
 #pragma unroll
   for (int i = 0; i < kTiles; ++i)
-    id[i] = table[min(first + i * kTileBlocks + r, n - 1)];
-  // column r: head r (beyond G the last again), dims 16 qd .. + 15 and 64 more
+    id[i] = table[min(first + i * kTileBlocks + r, P.max_blocks - 1)];
+  // row r: head r (beyond G the last again), dims 16 qd .. + 15 and 64 more
   uint32_t w[16];
   {
     const uint4* q = reinterpret_cast<const uint4*>(
@@ -298,9 +298,11 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
       w[4 * i + 3] = u.w;
     }
   }
+  const int n = L <= 0 ? 0 : min((L - 1) / kT + 1, P.max_blocks);
+  if (chunk * kScoreBlocks >= n) return;  // uniform
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
-    const bool ok = id[i] >= 0 && id[i] < P.nb;
+    const bool ok = first + i * kTileBlocks + r < n && id[i] >= 0 && id[i] < P.nb;
     id[i] = ok ? id[i] : 0;
     const i32x4* s = reinterpret_cast<const i32x4*>(sum + static_cast<int64_t>(id[i]) * kSum) + qd;
 #pragma unroll
@@ -339,8 +341,12 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
   __syncthreads();
   if (first >= n) return;  // uniform over the wavefront; no barrier follows
   i32x4 qb[4];
+  int eq4[4];  // of heads (rows) 4 qd ..
 #pragma unroll
-  for (int s = 0; s < 4; ++s) qb[s] = *reinterpret_cast<const i32x4*>(s_q[s][lane]);
+  for (int s = 0; s < 4; ++s) {
+    qb[s] = *reinterpret_cast<const i32x4*>(s_q[s][lane]);
+    eq4[s] = __shfl(eq, 4 * qd + s, 64);
+  }
   float* const to = P.scores + (static_cast<int64_t>(b) * P.H + g) * P.max_blocks;
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
@@ -348,34 +354,16 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int c
     if (row0 >= n) break;  // uniform over the wavefront
     i32x4 c = {0, 0, 0, 0};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i][j], qb[j], c, 0, 0, 0);
-    // the exponents of rows 4 qd .. 4 qd + 3: those of a quad of lanes in one
-    // word, then the word of quad qd
-    uint32_t quad = static_cast<uint32_t>(e[i]) & 255u;
-    const uint32_t pair = dpp<kXor1>(quad);
-    quad = r & 1 ? quad << 8 | pair : quad | pair << 8;
-    const uint32_t other = dpp<kXor2>(quad);
-    quad = r & 2 ? quad << 16 | other : quad | other << 16;
-    const uint32_t q0 = __builtin_amdgcn_readlane(quad, 0), q1 = __builtin_amdgcn_readlane(quad, 4);
-    const uint32_t q2 = __builtin_amdgcn_readlane(quad, 8), q3 = __builtin_amdgcn_readlane(quad, 12);
-    const uint32_t er4 = qd == 0 ? q0 : qd == 1 ? q1 : qd == 2 ? q2 : q3;
-    float v = 0.f;
-    int ev = 0;
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_i32_16x16x64_i8(qb[j], a[i][j], c, 0, 0, 0);
+    float v = -INFINITY;  // the largest of up to 16 heads
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int er = static_cast<int8_t>(er4 >> (8 * j));
-      // the largest column (of up to 16 heads)
-      float x = ldexpf(static_cast<float>(c[j]), er + eq);
-      auto larger = [](float p, uint32_t q) { return fmaxf(p, __uint_as_float(q)); };
-      x = larger(x, dpp<kXor1>(__float_as_uint(x)));
-      x = larger(x, dpp<kXor2>(__float_as_uint(x)));
-      x = larger(x, dpp<kXor7>(__float_as_uint(x)));
-      x = larger(x, dpp<kXor8>(__float_as_uint(x)));
-      v = r == j ? x : v;
-      ev = r == j ? er : ev;
-    }
-    if (r < 4 && row0 + 4 * qd + r < n)
-      to[row0 + 4 * qd + r] = ev == -128 ? -INFINITY : ev == kNotFinite ? INFINITY : v;
+    for (int j = 0; j < 4; ++j) v = fmaxf(v, ldexpf(static_cast<float>(c[j]), e[i] + eq4[j]));
+    if (G > 4)  // uniform: rows past the fourth are other heads
+      v = __uint_as_float(over_rows(__float_as_uint(v), [](uint32_t x, uint32_t y) {
+        return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
+      }));
+    if (qd == 0 && row0 + r < n)
+      to[row0 + r] = e[i] == -128 ? -INFINITY : e[i] == kNotFinite ? INFINITY : v;
   }
 }
 
