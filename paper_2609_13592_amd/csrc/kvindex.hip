@@ -31,7 +31,7 @@ typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 struct IndexParams {
-  const char* const* pt_k;  // this layer's K pages
+  bst::KPages pages;        // this layer's
   int8_t* sum;              // this layer's summaries [H][nb][256]
   int8_t* exp;              // and exponents [H][nb]
   const int32_t* tables;    // [B, max_blocks]
@@ -107,6 +107,11 @@ __device__ __forceinline__ uint32_t magnitude(i16x2 hi, i16x2 lo) {
   return max(one(h & 0xffffu, l & 0xffffu), one(h >> 16, l >> 16));
 }
 
+__device__ __forceinline__ const char* page_at(const bst::KPages& L, uint32_t page) {
+  const bool host = page >= L.first_host;
+  return (host ? L.host : L.hbm) + (static_cast<uint64_t>(host ? page - L.first_host : page) << 21);
+}
+
 // One wavefront per head-block.  FP4: lane (token r, group qd); else lane
 // (8-dim chunk r, token row qd of four).  Bound by the keys' bytes: the
 // extremes of two dims take one instruction, and no lane's value goes through
@@ -132,7 +137,7 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int ch
     if constexpr (FP4) {
       using namespace bst;
       const Fp4At f = fp4_at(g, id, P.nb);
-      const char* const page = P.pt_k[f.page];
+      const char* const page = page_at(P.pages, f.page);
       const uint4 c = *reinterpret_cast<const uint4*>(page + f.idx * kFp4Code + lane * 16);
       const float s = fp4_scale(
           static_cast<uint8_t>(page[kFp4ScaleAt + f.idx * kFp4Scale + lane]));
@@ -184,7 +189,8 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int ch
       if (lane == 0) P.exp[at] = static_cast<int8_t>(e);
     } else {
       const uint64_t byte = static_cast<uint64_t>(at) * kT * kD * 2;
-      const char* const src = P.pt_k[byte >> 21] + (byte & (bst::kPage - 1)) + lane * 16;
+      const char* const src = page_at(P.pages, static_cast<uint32_t>(byte >> 21)) +
+                              (byte & (bst::kPage - 1)) + lane * 16;
       u32x4 u[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)  // token 4 i + qd
@@ -591,15 +597,15 @@ int boost_kv_index_update(boost_ctx* ctx, const boost_kv_pool* p, int layer,
                           const int32_t* block_tables, int max_blocks, const int32_t* starts,
                           const int32_t* ends, int B, int max_tokens, void* stream) {
   if (!ctx || !p || !block_tables || !starts || !ends) return fail(BOOST_EINVAL, "null argument");
-  const char* const *pk, * const *pv;
-  if (int rc = kv_layer(p, layer, &pk, &pv)) return rc;
+  KPages pages;
+  if (int rc = k_pages(p, layer, pages)) return rc;
   if (!p->d_index) return fail(BOOST_EINVAL, "the pool has no block summaries");
   if (B < 1 || max_blocks < 1 || max_tokens < 1)
     return fail(BOOST_EINVAL, "B=%d max_blocks=%d max_tokens=%d", B, max_blocks, max_tokens);
   const int H = static_cast<int>(p->cfg.kv_heads);
   const uint64_t blocks = static_cast<uint64_t>(p->cfg.layers) * H * p->geom.nb;
   const uint64_t at = static_cast<uint64_t>(layer) * H * p->geom.nb;
-  const IndexParams P{pk, p->d_index + at * kSum, p->d_index + blocks * kSum + at, block_tables,
+  const IndexParams P{pages, p->d_index + at * kSum, p->d_index + blocks * kSum + at, block_tables,
                       starts, ends, B, H, static_cast<int>(p->geom.nb), max_blocks};
   // blocks that max_tokens new tokens can touch, one wavefront each (a
   // request with more has its wavefronts go round)

@@ -304,6 +304,15 @@ int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const ch
   return BOOST_OK;
 }
 
+int k_pages(const boost_kv_pool* p, int layer, KPages& at) {
+  const char* const *pk, * const *pv;
+  if (int rc = kv_layer(p, layer, &pk, &pv)) return rc;
+  const uint64_t host = p->geom.host_pages, hbm = p->geom.pages - host;
+  const char* const base = p->hbm.base + 2ull * layer * hbm * kPage;
+  at = {base, host ? p->host[layer].base : base, static_cast<uint32_t>(hbm)};
+  return BOOST_OK;
+}
+
 int kv_write4(const boost_kv_pool* p, int layer, const int32_t* slots, const int32_t* tables,
               int max_blocks, const int32_t* positions, const void* k, const void* v, int n,
               void* stream) {

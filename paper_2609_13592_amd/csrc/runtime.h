@@ -110,6 +110,17 @@ int kv_device(const boost_kv_pool* p);
 // Page tables of one layer's K and V (as kv_device, and EINVAL: layer).
 int kv_layer(const boost_kv_pool* p, int layer, const char* const** pk, const char* const** pv);
 
+// Where one layer's K pages lie: linear placement makes them a fixed function
+// of their number, [0, first_host) consecutive in the HBM slab and the rest in
+// the host slab, so a kernel needs no load from the page table before one from a
+// page.
+struct KPages {
+  const char *hbm, *host;
+  uint32_t first_host;
+};
+// (errors: as kv_layer)
+int k_pages(const boost_kv_pool* p, int layer, KPages& at);
+
 // n rows [H, 128] of K and V into a 4-bit pool, at the given slots or (slots
 // null) at the requests' positions; arguments checked by the caller.
 int kv_write4(const boost_kv_pool* p, int layer, const int32_t* slots, const int32_t* tables,
