@@ -354,8 +354,8 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
 #endif
 // SEL: the blocks of the KV head's list in place of the whole context (the
 // list's partial block may stand anywhere, so tokens are counted per block).
-// ONE: no list has more than one partition: a workgroup for every (KV head,
-// request), empty ones too, which writes the output rows itself.
+// ONE: no list has more than one partition: its workgroup writes the output
+// rows itself.  WAVE: which search finds a context's item (not for lists).
 template <int G, bool WAVE, bool SEL, bool ONE = false>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
     G == 8 || SEL ? 2 : BOOST_ATTN_WAVES))) void attn_partition(AttnParams P) {
@@ -372,11 +372,11 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   __shared__ int32_t s_tok[SEL ? kMaxPartBlocks : 1];  // tokens that count of each block
   __shared__ int s_red[4], s_pick[5];
   int part, b, g, L;
-  if constexpr (ONE) {
-    b = blockIdx.x % P.B;
-    g = P.H - 1 - blockIdx.x / P.B;
-    part = 0;
+  Listed entry;
+  if constexpr (SEL) {
+    item_each(P, b, g, part);
     L = P.lens[b];
+    entry = listed(P, b, g, part, tid);
   } else if constexpr (WAVE) {
     if (!item_of_wave(P, blockIdx.x, b, g, part, L)) return;  // uniform
   } else {
@@ -422,8 +422,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   // the partition's width of the table row (entries past the context are
   // read but not used)
   if constexpr (SEL) {
-    if (tid < nbp)
-      row[tid] = selected(P, b, g, blk_beg + tid, L, s_tok[tid]);
+    if (tid < nbp) row[tid] = selected(P, entry, L, s_tok[tid]);
   } else if (tid < min(P.part_blocks, P.max_blocks - blk_beg)) {
     row[tid] = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk_beg + tid];
   }
@@ -776,24 +775,22 @@ template <int G, bool SEL>
 int launch_partitions(AttnParams& P, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
   if (grid > 0x7fffffff) return bst::fail(BOOST_EINVAL, "grid too large");
+  dim3 g(static_cast<unsigned>(grid)), wg(kThreads);
   if constexpr (SEL) {
-    if (P.n_parts == 1) {
-      hipLaunchKernelGGL((attn_partition<G, true, true, true>), dim3(static_cast<unsigned>(grid)),
-                         dim3(kThreads), 0, s, P);
-      BOOST_HIP(hipGetLastError());
-      return BOOST_OK;
-    }
-  }
+    if (!grid_each(P, g)) return bst::fail(BOOST_EINVAL, "grid too large");
+    if (P.n_parts == 1)
+      hipLaunchKernelGGL((attn_partition<G, true, true, true>), g, wg, 0, s, P);
+    else
+      hipLaunchKernelGGL((attn_partition<G, true, true>), g, wg, 0, s, P);
   // up to 64 requests the search by wavefronts, in a kernel of its own (64
   // requests of 512..4096 tokens, 32 / 8 heads: 106.7 us, 108.4 with the search
   // by barriers, 111.0 with both in one kernel, whose registers spill; one of
   // 8192: 18.5 and 19.4)
-  if (P.B <= 64)
-    hipLaunchKernelGGL((attn_partition<G, true, SEL>), dim3(static_cast<unsigned>(grid)),
-                       dim3(kThreads), 0, s, P);
-  else
-    hipLaunchKernelGGL((attn_partition<G, false, SEL>), dim3(static_cast<unsigned>(grid)),
-                       dim3(kThreads), 0, s, P);
+  } else if (P.B <= 64) {
+    hipLaunchKernelGGL((attn_partition<G, true, SEL>), g, wg, 0, s, P);
+  } else {
+    hipLaunchKernelGGL((attn_partition<G, false, SEL>), g, wg, 0, s, P);
+  }
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

@@ -71,13 +71,12 @@ struct Block4 {
   int tok;      // tokens that count
 };
 
-// EIGHT: more than four query heads per KV head.  kOne: no context has more
-// than one partition: a workgroup for every (KV head, request), empty ones too.
-// W wavefronts (kWave and kGroup: 4, as the item search has it).
-enum class Items { kWave, kGroup, kOne };
+// EIGHT: more than four query heads per KV head.  W wavefronts (kWave and
+// kGroup, the searches: 4).  kEach: see item_each.
+enum class Items { kWave, kGroup, kEach };
 template <bool EIGHT, Items ITEMS, bool SEL, int W>
 __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
-  static_assert(ITEMS == Items::kOne || 64 * W == kThreads, "item search");
+  static_assert(ITEMS == Items::kEach || 64 * W == kThreads, "item search");
   __shared__ float s_acc[W][8][kAccRow];  // heads (EIGHT), else 4 heads of each part
   __shared__ float s_ml[W][8][2];
   __shared__ int32_t row[kMaxPartBlocks];    // the partition's pool blocks
@@ -90,23 +89,25 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
     if (!item_of(P, blockIdx.x, b, g, part, L, s_red, row, s_pick)) return;  // uniform
     __syncthreads();  // row has served the search
   } else {
-    b = blockIdx.x % P.B;
-    g = P.H - 1 - blockIdx.x / P.B;
-    part = 0;
+    item_each(P, b, g, part);
     L = P.lens[b];
   }
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  Listed entry;  // of a list: one a thread
+  if constexpr (SEL) entry = listed(P, b, g, part, tid);
   const int r = lane & 15, qd = lane >> 4;
   const int G = P.Hq / P.H;
   const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
   const int blk_beg = part * P.part_blocks;
+  if (ITEMS == Items::kEach && part > 0 && blk_beg >= n_blk) return;  // uniform
   const int nbp = min(n_blk, blk_beg + P.part_blocks) - blk_beg;
   const bool whole = n_blk <= P.part_blocks;
+  static_assert(!SEL || 64 * W >= kMaxPartBlocks, "a thread an entry");
   for (int i = tid; i < nbp; i += 64 * W) {
     int tok;
     int32_t blk;
     if constexpr (SEL) {
-      blk = selected(P, b, g, blk_beg + i, L, tok);
+      blk = selected(P, entry, L, tok);
     } else {
       blk = P.tables[static_cast<int64_t>(b) * P.max_blocks + blk_beg + i];
       tok = min(kT, L - (blk_beg + i) * kT);
@@ -326,31 +327,28 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
   }
 }
 
-template <bool EIGHT, Items ITEMS, int W>
-void launch(const AttnParams& P, unsigned grid, hipStream_t s) {
-  if (P.sel)
-    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, true, W>), dim3(grid), dim3(64 * W), 0, s, P);
-  else
-    hipLaunchKernelGGL((attn4_partition<EIGHT, ITEMS, false, W>), dim3(grid), dim3(64 * W), 0, s,
-                       P);
-}
-
 template <bool EIGHT>
-void launch(const AttnParams& P, unsigned grid, int n_cu, hipStream_t s) {
-  if (P.n_parts == 1) {
-    // a workgroup alone on its compute unit: a pair is one chain of products,
-    // maximum, exponentials and products, 83 ns a block with four wavefronts,
-    // 61 with eight (57 with 16: the unit's bandwidth); 32 requests of 1500
-    // tokens 12.4 us with eight and 13.9 with four, 64 of 1000 17.2 and 15.9
-    if (P.B * P.H <= n_cu)
-      launch<EIGHT, Items::kOne, 8>(P, grid, s);
-    else
-      launch<EIGHT, Items::kOne, 4>(P, grid, s);
-  } else if (P.B <= 64) {
-    launch<EIGHT, Items::kWave, 4>(P, grid, s);
-  } else {
-    launch<EIGHT, Items::kGroup, 4>(P, grid, s);
-  }
+void launch(const AttnParams& P, dim3 grid, int n_cu, hipStream_t s) {
+  auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, grid, dim3(threads), 0, s, P);
+  };
+  // a workgroup alone on its compute unit: a pair is one chain of products,
+  // maximum, exponentials and products, 83 ns a block with four wavefronts,
+  // 61 with eight (57 with 16: the unit's bandwidth); 32 requests of 1500
+  // tokens 12.4 us with eight and 13.9 with four, 64 of 1000 17.2 and 15.9
+  const bool alone = P.n_parts == 1 && P.B * P.H <= n_cu;
+  if (P.sel && alone)
+    go(attn4_partition<EIGHT, Items::kEach, true, 8>, 512);
+  else if (P.sel)
+    go(attn4_partition<EIGHT, Items::kEach, true, 4>, 256);
+  else if (alone)
+    go(attn4_partition<EIGHT, Items::kEach, false, 8>, 512);
+  else if (P.n_parts == 1)
+    go(attn4_partition<EIGHT, Items::kEach, false, 4>, 256);
+  else if (P.B <= 64)
+    go(attn4_partition<EIGHT, Items::kWave, false, 4>, 256);
+  else
+    go(attn4_partition<EIGHT, Items::kGroup, false, 4>, 256);
 }
 
 }  // namespace
@@ -360,11 +358,13 @@ namespace attn {
 
 int launch_fp4(AttnParams& P, int n_cu, hipStream_t s) {
   const int64_t grid = static_cast<int64_t>(P.H) * P.B * P.n_parts;
-  if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "grid too large");
+  dim3 g(static_cast<unsigned>(grid));
+  if (grid > 0x7fffffff || ((P.sel || P.n_parts == 1) && !grid_each(P, g)))
+    return fail(BOOST_EINVAL, "grid too large");
   if (P.Hq / P.H <= 4)
-    launch<false>(P, static_cast<unsigned>(grid), n_cu, s);
+    launch<false>(P, g, n_cu, s);
   else
-    launch<true>(P, static_cast<unsigned>(grid), n_cu, s);
+    launch<true>(P, g, n_cu, s);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }

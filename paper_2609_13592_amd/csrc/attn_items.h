@@ -292,15 +292,38 @@ __device__ inline bool item_of(const AttnParams& P, int idx, int& b, int& g, int
   return true;
 }
 
-// Pool block of entry i of the list of (request b, KV head g), L the request's
-// context length: -1 where the entry names no block of the context (its
-// tokens are left out); tok gets how many of its tokens lie inside.
-__device__ __forceinline__ int32_t selected(const AttnParams& P, int b, int g, int i, int L,
-                                            int32_t& tok) {
-  const int32_t at = P.sel[(static_cast<int64_t>(b) * P.H + g) * P.top_k + i];
-  const bool in = at >= 0 && at < P.max_blocks && at <= (L - 1) / kT;
-  tok = in ? min(kT, L - at * kT) : 0;
-  return in ? P.tables[static_cast<int64_t>(b) * P.max_blocks + at] : -1;
+// Work item of a call over lists, or of one whose contexts have one partition:
+// a grid of requests, KV heads and partitions, the empty ones too.  Nothing is
+// read or divided for it, and lists differ little in length.
+__device__ __forceinline__ void item_each(const AttnParams& P, int& b, int& g, int& part) {
+  b = blockIdx.x;
+  g = P.H - 1 - static_cast<int>(blockIdx.y);
+  part = blockIdx.z;
+}
+// (false: more than a grid holds)
+inline bool grid_each(const AttnParams& P, dim3& grid) {
+  grid = dim3(P.B, P.H, P.n_parts);
+  return P.H <= 65535 && P.n_parts <= 65535;
+}
+
+// Entry i of partition `part` of the list of (request b, KV head g), past its
+// end the last: its index in the context and the pool block there, loaded
+// without waiting for the context's length (and by every thread: behind a branch
+// on the thread the compiler took the partition for one of the thread's own).
+struct Listed {
+  int32_t at, block;
+};
+__device__ __forceinline__ Listed listed(const AttnParams& P, int b, int g, int part, int i) {
+  const int k = min(part * P.part_blocks + min(i, P.part_blocks - 1), P.top_k - 1);
+  const int32_t at = P.sel[(static_cast<int64_t>(b) * P.H + g) * P.top_k + k];
+  return {at, P.tables[static_cast<int64_t>(b) * P.max_blocks + min(max(at, 0), P.max_blocks - 1)]};
+}
+// ... as a context of L tokens has it: -1 where the entry names no block of it
+// (its tokens are left out); tok gets how many of its tokens lie inside.
+__device__ __forceinline__ int32_t selected(const AttnParams& P, const Listed& e, int L, int32_t& tok) {
+  const bool in = e.at >= 0 && e.at < P.max_blocks && e.at <= (L - 1) / kT;
+  tok = in ? min(kT, L - e.at * kT) : 0;
+  return in ? e.block : -1;
 }
 
 // The kernels of a 4-bit pool: launches the partitions (any Hq / H up to 8).
