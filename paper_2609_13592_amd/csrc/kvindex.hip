@@ -115,7 +115,9 @@ __device__ __forceinline__ const char* page_at(const bst::KPages& L, uint32_t pa
 // One wavefront per head-block.  FP4: lane (token r, group qd); else lane
 // (8-dim chunk r, token row qd of four).  Bound by the keys' bytes: the
 // extremes of two dims take one instruction, and no lane's value goes through
-// LDS.
+// LDS.  104 MB of keys (four prompts of 9001..16384 tokens, 8 heads, bf16): 22
+// us, 4.7 TB/s (33 through LDS; two blocks a wavefront at a time 2 us more); the
+// last blocks of 16 requests 3.6.
 template <bool FP4>
 __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int chunks) {
   const int lane = threadIdx.x & 63, r = lane & 15, qd = lane >> 4;
@@ -267,7 +269,8 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
 // the negative one), so that a lane ends with four heads of one block.  Bound by
 // the summaries' bytes and the chain before them (block ids): the loads of all
 // four tiles are out together, and q is rounded while they are, a quarter by
-// each wavefront.
+// each wavefront.  33 MB (16 requests of 2000..30000 tokens, 8 heads) 11.8 us,
+// one of 131072 tokens 4.8.
 constexpr int kTileBlocks = 16, kTiles = 4;
 constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
@@ -394,7 +397,8 @@ __device__ __forceinline__ int wave_scan(int v) {
 // wavefronts between its barriers, not by the 4 bytes a block: nothing
 // branches on a key, a digit is one barrier (every wavefront sums the counters
 // for itself) and has counters of its own, four of each so that equal digits
-// do not all wait for one another.
+// do not all wait for one another.  8 lists of 128 among 8192 blocks 6.9 us
+// (12.5 with two barriers and branches), 128 of 64 among up to 1875 5.1.
 template <int NT, int V>
 __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   constexpr int kWaves = NT / 64, kRound = 64;  // chunks of NT keys ranked at a time
