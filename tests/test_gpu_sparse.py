@@ -444,6 +444,97 @@ def test_every_block_gives_the_dense_result(gpu_ctx, fmt):
         c.close()
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_offsets_past_32_bits(gpu_ctx, fmt):
+    """Tensors of more than 4 GiB each (two layers, the second used): the last
+    blocks of the pool written, read, summarised, copied and attended to."""
+    rng = np.random.default_rng(11)
+    big = 160000 if fmt == bd.KV_BF16 else 540000
+    c = Cache(gpu_ctx, rng, fmt, [900, 33, 1], 8, 32, extra=big, layers=2, layer=1)
+    try:
+        pages = bd.boost_kv_pages(c.pool, 1, 0)
+        assert int(pages[-1]) - int(pages[0]) > 2 ** 32
+        need = [(int(L) + 15) // 16 for L in c.lens]
+        ids = c.nb - 1 - rng.permutation(sum(need))
+        for b in range(3):
+            at = sum(need[:b])
+            c.tables[b, :need[b]] = ids[at:at + need[b]]
+        c.write()
+        bd.boost_kv_index_enable(c.pool)
+        c.index()
+        sel = c.check_selection(20, 1, 1)
+        whole = np.tile(np.arange(c.mb, dtype=np.int32), (3, 8, 1))
+        o, dense = c.attend(sel), dev_f32(3, 32, 128)
+        c.check_attention(o, sel)
+
+        def attend_all():
+            bd.boost_paged_attn_decode(gpu_ctx, c.pool, 1, to_dev_u16(c.q), 3, 32, dev_i32(c.tables), c.mb,
+                                       dev_i32(c.lens), 0.0, dense, bd.DTYPE_F32, stream())
+            sync()
+            return dense.cpu().numpy()
+        d = attend_all()
+        c.check_attention(d, whole)
+        for b, L in enumerate(c.lens):
+            t = np.arange(int(L))
+            k, v = dev_u16(int(L), 8, 128), dev_u16(int(L), 8, 128)
+            bd.boost_kv_read(gpu_ctx, c.pool, 1, dev_i32(c.tables[b, t // 16] * 16 + t % 16), k, v, int(L),
+                             stream())
+            sync()
+            assert np.array_equal(og.bf16_to_f32(host_u16(k)).astype(np.float64), c.meaning(c.k[b]))
+            assert np.array_equal(og.bf16_to_f32(host_u16(v)).astype(np.float64), c.meaning(c.v[b]))
+        # the same blocks elsewhere: every bit the same
+        to = c.nb - 1000 - ids[::-1]
+        to = to - to.min() + c.nb // 2
+        bd.boost_kv_copy_blocks(gpu_ctx, c.pool, 0, 2, ids, to, len(ids), stream())
+        new = dict(zip(ids.tolist(), to.tolist()))
+        c.tables = np.where(c.tables >= 0, np.vectorize(lambda i: new.get(i, -1))(c.tables), -1).astype(np.int32)
+        assert np.array_equal(c.check_selection(20, 1, 1), sel)
+        assert np.array_equal(c.attend(sel), o)
+        assert np.array_equal(attend_all(), d)
+    finally:
+        c.close()
+
+
+def test_two_pools_on_two_streams(gpu_ctx):
+    """A pool of each format, each on a stream of its own, their calls in turn
+    and nothing waited for in between: the results of either one alone."""
+    import torch
+    cs, want, runs = [], [], []
+    try:
+        for fmt in FORMATS:
+            c = Cache(gpu_ctx, np.random.default_rng(20 + fmt), fmt, [3000, 17, 640, 0], 8, 32)
+            cs.append(c)
+            c.write()
+            bd.boost_kv_index_enable(c.pool)
+            c.index()
+            _, sel = c.select(24, 1, 1)
+            want.append((sel, c.attend(sel)))
+        for c in cs:
+            st = torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                t, ln, q = dev_i32(c.tables), dev_i32(c.lens), to_dev_u16(c.q)
+                sc = torch.zeros((4, 8, c.mb), dtype=torch.float32, device="cuda")
+                sel = torch.full((4, 8, 24), 99, dtype=torch.int32, device="cuda")
+                out = torch.full((4, 32, 128), float("nan"), device="cuda")
+                zero = dev_i32([0] * 4)
+            runs.append((c, st, t, ln, q, sc, sel, out, zero))
+        sync()
+        for _ in range(20):
+            for c, st, t, ln, q, sc, sel, out, zero in runs:
+                s = st.cuda_stream
+                bd.boost_kv_index_update(gpu_ctx, c.pool, 0, t, c.mb, zero, ln, 4, 3000, s)
+                bd.boost_kv_select(gpu_ctx, c.pool, 0, q, 4, 32, t, c.mb, ln, 24, 1, 1, sc, sel, s)
+                bd.boost_sparse_attn_decode(gpu_ctx, c.pool, 0, q, 4, 32, t, c.mb, ln, sel, 24, 0.0, out,
+                                            bd.DTYPE_F32, s)
+        sync()
+        for r, (sel, o) in zip(runs, want):
+            assert np.array_equal(r[6].cpu().numpy(), sel)
+            assert np.array_equal(r[7].cpu().numpy(), o)
+    finally:
+        for c in cs:
+            c.close()
+
+
 def test_wide_groups_select(gpu_ctx):
     """Selection takes up to 16 query heads per KV head."""
     rng = np.random.default_rng(10)
