@@ -115,14 +115,13 @@ __device__ __forceinline__ const char* page_at(const bst::KPages& L, uint32_t pa
 // One wavefront per head-block.  FP4: lane (token r, group qd); else lane
 // (8-dim chunk r, token row qd of four).  Bound by the keys' bytes: the
 // extremes of two dims take one instruction, and no lane's value goes through
-// LDS.  104 MB of keys (four prompts of 9001..16384 tokens, 8 heads, bf16): 22
+// LDS.  104 MB of keys (four prompts of 9001..16384 tokens, 8 heads, bf16): 21
 // us, 4.7 TB/s (33 through LDS; two blocks a wavefront at a time 2 us more); the
 // last blocks of 16 requests 3.6.
 template <bool FP4>
-__global__ __launch_bounds__(256) void index_update_kernel(IndexParams P, int chunks) {
+__global__ __launch_bounds__(256) void index_update_kernel(IndexParams P) {
   const int lane = threadIdx.x & 63, r = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x % chunks, bg = blockIdx.x / chunks;
-  const int g = bg % P.H, b = bg / P.H;
+  const int b = blockIdx.z, g = blockIdx.y, chunk = blockIdx.x, chunks = gridDim.x;
   const int start = max(P.starts[b], 0);
   const int end = static_cast<int>(
       min(static_cast<int64_t>(P.ends[b]), static_cast<int64_t>(P.max_blocks) * kT));
@@ -274,13 +273,12 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
 constexpr int kTileBlocks = 16, kTiles = 4;
 constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
-__global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P, int chunks) {
+__global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
   // the operand of q by lane: dword w of 16 dims of step s (positive parts of
   // the lower and the upper 64 dims, then the negative ones)
   __shared__ uint32_t s_q[4][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
-  const int chunk = blockIdx.x % chunks, bg = blockIdx.x / chunks;
-  const int g = bg % P.H, b = bg / P.H;
+  const int b = blockIdx.z, g = blockIdx.y, chunk = blockIdx.x;
   const int L = P.lens[b];  // (the ids do not wait for it)
   const int first = chunk * kScoreBlocks + wave * kTiles * kTileBlocks;
   const int G = P.Hq / P.H;
@@ -616,12 +614,10 @@ int boost_kv_index_update(boost_ctx* ctx, const boost_kv_pool* p, int layer,
   const int64_t touched = std::min<int64_t>((static_cast<int64_t>(max_tokens) + 2 * kT - 2) / kT,
                                             max_blocks);
   const int chunks = static_cast<int>((touched + 3) / 4);
-  const int64_t grid = static_cast<int64_t>(chunks) * B * H;
-  if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "grid too large");
+  if (H > 65535 || B > 65535) return fail(BOOST_EINVAL, "grid too large");
   const auto kernel = p->format == BOOST_KV_FP4 ? index_update_kernel<true>
                                                 : index_update_kernel<false>;
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
-                     static_cast<hipStream_t>(stream), P, chunks);
+  hipLaunchKernelGGL(kernel, dim3(chunks, H, B), dim3(256), 0, static_cast<hipStream_t>(stream), P);
   BOOST_HIP(hipGetLastError());
   return BOOST_OK;
 }
@@ -649,11 +645,10 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
                        static_cast<const uint16_t*>(q), block_tables, ctx_lens, scores, sel, B, H,
                        Hq, static_cast<int>(p->geom.nb), max_blocks, top_k, n_first, n_last};
   const int chunks = (max_blocks + kScoreBlocks - 1) / kScoreBlocks;
-  const int64_t grid = static_cast<int64_t>(chunks) * B * H;
-  if (grid > 0x7fffffff) return fail(BOOST_EINVAL, "grid too large");
+  if (H > 65535 || B > 65535 || static_cast<int64_t>(B) * H > 0x7fffffff)
+    return fail(BOOST_EINVAL, "grid too large");
   const auto s = static_cast<hipStream_t>(stream);
-  hipLaunchKernelGGL(block_scores_kernel, dim3(static_cast<unsigned>(grid)), dim3(256), 0, s, P,
-                     chunks);
+  hipLaunchKernelGGL(block_scores_kernel, dim3(chunks, H, B), dim3(256), 0, s, P);
   BOOST_HIP(hipGetLastError());
   // keys in registers as far as they go, and no more wavefronts than have work
   // (whole steps: 64 requests of 250 blocks 46.5 us with 256 threads, 48.4 with

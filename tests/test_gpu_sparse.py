@@ -593,13 +593,18 @@ def test_refusals(gpu_ctx):
         bd.boost_kv_pool_destroy(small)
 
 
-def test_lists_too_long(gpu_ctx):
+def test_lists_and_batches_too_long(gpu_ctx):
     import torch
     pool = bd.boost_kv_pool_create(gpu_ctx, 1, 2, 128, 100, 0, bd.KV_ALL_HBM, q_heads=8, max_batch=1,
                                    max_blocks_per_seq=8)
     try:
         bd.boost_kv_index_enable(pool)
         z = torch.zeros(8 * 128, dtype=torch.int32, device="cuda")
+        for f in (lambda: bd.boost_kv_select(gpu_ctx, pool, 0, z, 65536, 8, z, 8, z, 4, 0, 0, z, z, stream()),
+                  lambda: bd.boost_kv_index_update(gpu_ctx, pool, 0, z, 8, z, z, 65536, 1, stream())):
+            with pytest.raises(bd.BoostError) as e:
+                f()
+            assert e.value.code == bd.EINVAL
         for top in (2 ** 27 + 1, 2 ** 31 - 1):
             for f in (lambda: bd.boost_kv_select(gpu_ctx, pool, 0, z, 1, 8, z, 8, z, top, 0, 0, z, z, stream()),
                       lambda: bd.boost_sparse_attn_decode(gpu_ctx, pool, 0, z, 1, 8, z, 8, z, z, top, 0.0, z,
