@@ -656,7 +656,8 @@ int boost_kv_index_enable(boost_kv_pool *pool);
  * its keys scores +inf.  starts, ends: device int32 [B].  max_tokens is the
  * largest ends - starts (it sizes the launch; larger ranges are done all the
  * same).  Two requests must not update the same block in one call with other
- * ends.  B up to 65535, here and in boost_kv_select.  Errors: EINVAL (also: no summaries), ENODEV, EHIP. */
+ * ends.  B up to 65535, here and in boost_kv_select.
+ * Errors: EINVAL (also: no summaries), ENODEV, EHIP. */
 int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
                           const int32_t *block_tables, int max_blocks,
                           const int32_t *starts, const int32_t *ends, int B,

@@ -18,8 +18,9 @@ int kv_geometry(uint32_t n_blocks, uint32_t H, uint32_t D, uint32_t T, uint32_t 
   if (mode == BOOST_KV_BUDGET && layers == 0) return fail(BOOST_EINVAL, "0 layers");
   if (mode == BOOST_KV_LPP && M < 2) return fail(BOOST_EINVAL, "M=%u < 2", M);
   const uint64_t hbb = static_cast<uint64_t>(T) * D * 2;  // one head of one block
-  if (!blocks_per_page && kPage % hbb) return fail(BOOST_EINVAL, "head-block of %llu B does not divide a page",
-                               (unsigned long long)hbb);
+  if (!blocks_per_page && kPage % hbb)
+    return fail(BOOST_EINVAL, "head-block of %llu B does not divide a page",
+                (unsigned long long)hbb);
   g = KvGeom{};
   g.H = H;
   g.D = D;

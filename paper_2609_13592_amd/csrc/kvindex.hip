@@ -94,6 +94,13 @@ __device__ __forceinline__ uint32_t over_rows(uint32_t v, F f) {
   return f(b[0], b[1]);
 }
 
+template <typename F>
+__device__ __forceinline__ i16x2 over_rows2(i16x2 v, F f) {
+  return __builtin_bit_cast(i16x2, over_rows(__builtin_bit_cast(uint32_t, v), [&](uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, f(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
+  }));
+}
+
 // The larger magnitude, as bf16 bits, of extremes hi (largest) and lo
 // (smallest) in both halves.
 __device__ __forceinline__ uint32_t magnitude(i16x2 hi, i16x2 lo) {
@@ -215,12 +222,8 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P) {
       uint32_t amax = 0;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        mx[j] = __builtin_bit_cast(i16x2, over_rows(__builtin_bit_cast(uint32_t, mx[j]), [](uint32_t a, uint32_t b) {
-          return __builtin_bit_cast(uint32_t, max2(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
-        }));
-        mn[j] = __builtin_bit_cast(i16x2, over_rows(__builtin_bit_cast(uint32_t, mn[j]), [](uint32_t a, uint32_t b) {
-          return __builtin_bit_cast(uint32_t, min2(__builtin_bit_cast(i16x2, a), __builtin_bit_cast(i16x2, b)));
-        }));
+        mx[j] = over_rows2(mx[j], max2);
+        mn[j] = over_rows2(mn[j], min2);
         amax = max(amax, magnitude(mx[j], mn[j]));
       }
       amax = row_max(amax);

@@ -1,7 +1,8 @@
 // KV pool (§4.2 LPP, §4.5 heads-outermost layout and two free lists) and the
 // kernels that write its tokens and read them back.  Every layer has a K and
-// a V tensor [H][NB][T][D], bf16 or in 4 bits (kvfmt.h); the LPP tail pages of each tensor live in pinned host memory, the rest in
-// one HBM slab; the device page table maps (layer, K/V, page) to an address.
+// a V tensor [H][NB][T][D], bf16 or in 4 bits (kvfmt.h); the LPP tail pages of
+// each tensor live in pinned host memory, the rest in one HBM slab; the device
+// page table maps (layer, K/V, page) to an address.
 #include <algorithm>
 #include <cstring>
 #include <exception>
