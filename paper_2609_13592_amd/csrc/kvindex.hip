@@ -276,14 +276,18 @@ __device__ __forceinline__ int context_blocks(const SelectParams& P, int b) {
 constexpr int kTileBlocks = 16, kTiles = 4;
 constexpr int kScoreBlocks = 4 * kTileBlocks * kTiles;  // per workgroup
 
-__global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
+// A workgroup's (4 or 8 wavefronts') share of the scores of (request b, KV head
+// g): blocks from `base` on, to P.scores and, if not null, s_score[block].
+// Returns the context's blocks.
+__device__ __forceinline__ int scores_from(const SelectParams& P, int b, int g, int base,
+                                           float* s_score) {
   // the operand of q by lane: dword w of 16 dims of step s (positive parts of
   // the lower and the upper 64 dims, then the negative ones)
   __shared__ uint32_t s_q[4][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
-  const int b = blockIdx.z, g = blockIdx.y, chunk = blockIdx.x;
+  const int quarter = wave & 3;  // of the rounding of q (of eight wavefronts two do each)
   const int L = P.lens[b];  // (the ids do not wait for it)
-  const int first = chunk * kScoreBlocks + wave * kTiles * kTileBlocks;
+  const int first = base + wave * kTiles * kTileBlocks;
   const int G = P.Hq / P.H;
   const int8_t* const sum = P.sum + static_cast<int64_t>(g) * P.nb * kSum;
   const int8_t* const exps = P.exp + static_cast<int64_t>(g) * P.nb;
@@ -309,7 +313,7 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
     }
   }
   const int n = L <= 0 ? 0 : min((L - 1) / kT + 1, P.max_blocks);
-  if (chunk * kScoreBlocks >= n) return;  // uniform
+  if (base >= n) return n;  // uniform
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
     const bool ok = first + i * kTileBlocks + r < n && id[i] >= 0 && id[i] < P.nb;
@@ -332,8 +336,8 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
     uint32_t x0 = w[8 * h], x1 = w[8 * h + 1];
 #pragma unroll
     for (int i = 1; i < 4; ++i) {
-      x0 = wave == i ? w[8 * h + 2 * i] : x0;
-      x1 = wave == i ? w[8 * h + 2 * i + 1] : x1;
+      x0 = quarter == i ? w[8 * h + 2 * i] : x0;
+      x1 = quarter == i ? w[8 * h + 2 * i + 1] : x1;
     }
     // whole numbers up to 127 by the rule of eq; the conversion has 0 for
     // what is below 0
@@ -345,11 +349,11 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
       pos = __builtin_amdgcn_cvt_pk_u8_f32(f[j], j, pos);
       neg = __builtin_amdgcn_cvt_pk_u8_f32(-f[j], j, neg);
     }
-    s_q[h][lane][wave] = none ? 0 : pos;
-    s_q[2 + h][lane][wave] = none ? 0 : neg;
+    s_q[h][lane][quarter] = none ? 0 : pos;
+    s_q[2 + h][lane][quarter] = none ? 0 : neg;
   }
   __syncthreads();
-  if (first >= n) return;  // uniform over the wavefront; no barrier follows
+  if (first >= n) return n;  // uniform over the wavefront; no barrier follows
   i32x4 qb[4];
   int eq4[4];  // of heads (rows) 4 qd ..
 #pragma unroll
@@ -372,9 +376,17 @@ __global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
       v = __uint_as_float(over_rows(__float_as_uint(v), [](uint32_t x, uint32_t y) {
         return __float_as_uint(fmaxf(__uint_as_float(x), __uint_as_float(y)));
       }));
-    if (qd == 0 && row0 + r < n)
-      to[row0 + r] = e[i] == -128 ? -INFINITY : e[i] == kNotFinite ? INFINITY : v;
+    v = e[i] == -128 ? -INFINITY : e[i] == kNotFinite ? INFINITY : v;
+    if (qd == 0 && row0 + r < n) {
+      to[row0 + r] = v;
+      if (s_score) s_score[row0 + r] = v;
+    }
   }
+  return n;
+}
+
+__global__ __launch_bounds__(256) void block_scores_kernel(SelectParams P) {
+  scores_from(P, blockIdx.z, blockIdx.y, blockIdx.x * kScoreBlocks, nullptr);
 }
 
 // Sum of v over this lane and those before it.
@@ -400,8 +412,9 @@ __device__ __forceinline__ int wave_scan(int v) {
 // for itself) and has counters of its own, four of each so that equal digits
 // do not all wait for one another.  8 lists of 128 among 8192 blocks 6.9 us
 // (12.5 with two barriers and branches), 128 of 64 among up to 1875 5.1.
-template <int NT, int V>
-__global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
+// score(i): that of block i of n; list: its number among [B, H].
+template <int NT, int V, typename Score>
+__device__ __forceinline__ void select_list(const SelectParams& P, int64_t list, int n, Score score) {
   constexpr int kWaves = NT / 64, kRound = 64;  // chunks of NT keys ranked at a time
   constexpr int kCopies = 4, kDigits = 4, kCounters = 256 * kCopies;
   // of each digit, and 64 that nothing reads, for keys that do not count
@@ -409,27 +422,24 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   __shared__ int s_cnt[kRound * (kWaves + 1)];  // above | equal << 16, of a chunk's wavefronts
   __shared__ uint32_t s_bits[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b = blockIdx.x / P.H;
-  const int n = context_blocks(P, b);
-  int32_t* const sel = P.sel + static_cast<int64_t>(blockIdx.x) * P.top_k;
+  int32_t* const sel = P.sel + list * P.top_k;
   if (n <= P.top_k) {  // uniform: every block
     for (int i = tid; i < P.top_k; i += NT) sel[i] = i < n ? i : -1;
     return;
   }
-  const float* const scores = P.scores + static_cast<int64_t>(blockIdx.x) * P.max_blocks;
   // the key of blocks that are always taken; no score's (it would be a NaN's)
   constexpr uint32_t kAlways = 0xffffffffu;
-  auto key_of = [&](float score, int i) {
-    const uint32_t u = __float_as_uint(score + 0.f);  // -0 as 0: they are equal
+  auto key_of = [&](float v, int i) {
+    const uint32_t u = __float_as_uint(v + 0.f);  // -0 as 0: they are equal
     const uint32_t k = u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
     return i < P.n_first || i >= n - P.n_last ? kAlways : k;
   };
-  auto key_at = [&](int i) { return key_of(scores[i], i); };
+  auto key_at = [&](int i) { return key_of(score(i), i); };
   const int chunks = (n + NT - 1) / NT;
   uint32_t key[V];
   float own[V];  // loaded without a branch, all of them together
 #pragma unroll
-  for (int j = 0; j < V; ++j) own[j] = scores[min(j * NT + tid, n - 1)];
+  for (int j = 0; j < V; ++j) own[j] = score(min(j * NT + tid, n - 1));
   for (int i = tid; i < kDigits * kCounters / 4; i += NT)
     reinterpret_cast<i32x4*>(hist)[i] = i32x4{0, 0, 0, 0};
 #pragma unroll
@@ -571,6 +581,26 @@ __global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
   }
 }
 
+template <int NT, int V>
+__global__ __launch_bounds__(NT) void select_blocks_kernel(SelectParams P) {
+  const float* const scores = P.scores + static_cast<int64_t>(blockIdx.x) * P.max_blocks;
+  select_list<NT, V>(P, blockIdx.x, context_blocks(P, blockIdx.x / P.H),
+                     [&](int i) { return scores[i]; });
+}
+
+// Both in one launch, for tables whose scores one workgroup of W wavefronts
+// computes in a round.
+template <int W>
+__global__ __launch_bounds__(64 * W) void scores_select_kernel(SelectParams P) {
+  constexpr int kBlocks = W * kTiles * kTileBlocks;
+  __shared__ float s_score[kBlocks];
+  const int g = blockIdx.x, b = blockIdx.y;
+  const int n = scores_from(P, b, g, 0, s_score);
+  __syncthreads();
+  select_list<64 * W, kBlocks / (64 * W)>(P, static_cast<int64_t>(b) * P.H + g, n,
+                                          [&](int i) { return s_score[i]; });
+}
+
 }  // namespace
 
 using namespace bst;
@@ -651,17 +681,27 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   if (H > 65535 || B > 65535 || static_cast<int64_t>(B) * H > 0x7fffffff)
     return fail(BOOST_EINVAL, "grid too large");
   const auto s = static_cast<hipStream_t>(stream);
+  // Tables of up to 512 blocks in one launch (whole steps: one request of 250
+  // blocks 17.9 us, 19.5 with two launches; 64 of 250 43.6 and 45.6; 24 of 500
+  // in 4 bits 20.5 and 22.1, four of them 18.9 and 18.2).  1000 blocks to a
+  // workgroup: one request 25.9 and 20.4.
+  if (max_blocks <= 512) {
+    if (max_blocks <= 256)
+      hipLaunchKernelGGL(scores_select_kernel<4>, dim3(H, B), dim3(256), 0, s, P);
+    else
+      hipLaunchKernelGGL(scores_select_kernel<8>, dim3(H, B), dim3(512), 0, s, P);
+    BOOST_HIP(hipGetLastError());
+    return BOOST_OK;
+  }
   hipLaunchKernelGGL(block_scores_kernel, dim3(chunks, H, B), dim3(256), 0, s, P);
   BOOST_HIP(hipGetLastError());
   // keys in registers as far as they go, and no more wavefronts than have work
-  // (whole steps: 64 requests of 250 blocks 46.5 us with 256 threads, 48.4 with
-  // 512; 16 of up to 1875 blocks 44.8 with 512, 46.2 with 1024; one of 8192 28.1
-  // with 512, 28.8 with 1024 and 30.6 with 256; one of 31250 45.5 with 32 keys a
-  // thread, 54.5 with 16 and the rest read again in every pass)
+  // (whole steps: 16 requests of up to 1875 blocks 44.8 us with 512 threads, 46.2
+  // with 1024; one of 8192 28.1 with 512, 28.8 with 1024 and 30.6 with 256; one
+  // of 31250 45.5 with 32 keys a thread, 54.5 with 16 and the rest read again in
+  // every pass)
   const dim3 rows(static_cast<unsigned>(B) * H);
-  if (max_blocks <= 512)
-    hipLaunchKernelGGL((select_blocks_kernel<256, 2>), rows, dim3(256), 0, s, P);
-  else if (max_blocks <= 2048)
+  if (max_blocks <= 2048)
     hipLaunchKernelGGL((select_blocks_kernel<512, 4>), rows, dim3(512), 0, s, P);
   else if (max_blocks <= 8192)
     hipLaunchKernelGGL((select_blocks_kernel<512, 16>), rows, dim3(512), 0, s, P);

@@ -249,7 +249,7 @@ def test_sizes(gpu_ctx, fmt, B, hi):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("n", [512, 2048, 8193, 32769, 70001])
+@pytest.mark.parametrize("n", [200, 256, 257, 512, 513, 2048, 5000, 8193, 32769, 70001])
 def test_selection_over_tables_of_every_width(gpu_ctx, fmt, n):
     """Tables that name each of 300 blocks (and some that are none) many times:
     many equal scores, and every way a workgroup holds the keys."""
