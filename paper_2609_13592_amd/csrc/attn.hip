@@ -669,14 +669,16 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
     }
 #pragma unroll
     for (int u = 0; u < kMergeBatch; ++u) {
-      if (mp[u] == -INFINITY) continue;  // past np, or an empty partition
+      // past np, or an empty partition (one of NaN scores alone has that
+      // maximum too, and a NaN sum)
+      if (mp[u] == -INFINITY && lp[u] == 0.f) continue;
       const float w = __builtin_amdgcn_exp2f(mp[u] - M);  // maxima are in the log2 domain
       den = fmaf(lp[u], w, den);
       o0 = fmaf(a[u].x, w, o0);
       o1 = fmaf(a[u].y, w, o1);
     }
   }
-  const float inv = den > 0.f ? 1.f / den : 0.f;
+  const float inv = den != 0.f ? 1.f / den : 0.f;  // NaN stays one
   const int64_t oi = static_cast<int64_t>(bh) * kD + lane * 2;
   if (P.out_bf16) {
     uint16_t* o = static_cast<uint16_t*>(P.out) + oi;
@@ -723,13 +725,16 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d, 64));
     M = fmaxf(M, m);
-    if (M == -INFINITY) continue;  // uniform: nothing but empty partitions
+    // a partition whose scores are all NaN: its maximum says nothing (lowest,
+    // as an empty one's), its sum is NaN
+    const bool nan = ml.y != ml.y;
+    if (M == -INFINITY && !__any(nan)) continue;  // uniform: nothing but empty partitions
     const float c = __builtin_amdgcn_exp2f(m - M);  // m = -inf: 0
     den *= c;
     o0 *= c;
     o1 *= c;
     m = M;
-    const float w = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float w = nan ? ml.y : ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
     const float wl = w * ml.y;
     for (int u0 = 0; u0 < n; u0 += kBatch) {
       if (u0 > 0) load(u0);
@@ -759,7 +764,8 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
   den = o0 = o1 = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    const float c = s_m[w] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s_m[w] - M);
+    const float c = s_m[w] == -INFINITY && s_den[w] == 0.f ? 0.f
+                                                           : __builtin_amdgcn_exp2f(s_m[w] - M);
     den = fmaf(s_den[w], c, den);
     o0 = fmaf(s_o[w][lane].x, c, o0);
     o1 = fmaf(s_o[w][lane].y, c, o1);
