@@ -141,6 +141,14 @@ __device__ __forceinline__ uint4 live(const uint4& v, bool valid) {
   return make_uint4(valid ? v.x : 0, valid ? v.y : 0, valid ? v.z : 0, valid ? v.w : 0);
 }
 
+// A score in the log2 domain, rounded by itself: the largest minus itself is then
+// 0 at any size.  (Fused into the subtraction of the maximum, what is left is the
+// maximum's own rounding, past 2^31 more than exp2 holds.)
+__device__ __forceinline__ float scaled(float dot, float sc2) {
+#pragma clang fp contract(off)
+  return dot * sc2;
+}
+
 // Online-softmax update of one token slot with U blocks.  Scores are in the
 // log2 domain (q . k * scale * log2 e), so exp2 is one instruction.  With
 // MASKED false every token is valid; otherwise invalid tokens have score -inf
@@ -158,7 +166,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
       d = dot2(qp[j][1], kb[u].y, d);
       d = dot2(qp[j][2], kb[u].z, d);
       d = dot2(qp[j][3], kb[u].w, d);
-      d = row16_sum(d) * sc2;  // q . k over the 16 lanes of the token row
+      d = scaled(row16_sum(d), sc2);  // q . k over the 16 lanes of the token row
       sc[u][j] = (!MASKED || valid[u]) ? d : -INFINITY;
     }
   after_k();  // the K registers are free from here on
@@ -270,7 +278,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
         x = dot2(q[j].z, kb[u].z, x);
         d[j] = dot2(q[j].w, kb[u].w, x);
       }
-      const float f = score_of_lane_head<Q>(d, b0, b1) * sc2;
+      const float f = scaled(score_of_lane_head<Q>(d, b0, b1), sc2);
       s[u][i] = (!MASKED || valid[u]) ? f : -INFINITY;
     }
     if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);  // (registers)

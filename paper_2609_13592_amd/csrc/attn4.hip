@@ -159,6 +159,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
   };
   const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
   auto scores = [&](const Block4& x) {
+#pragma clang fp contract(off)
     const float ks = bst::fp4_scale(x.ks);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -167,7 +168,10 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
                        fp4_unpack<2>(x.k[i], ks), fp4_unpack<3>(x.k[i], ks)};
       s = mfma(a, bq[i], s);
     }
-    return s;
+    // rounded by itself, so that the largest minus itself is 0 at any size (fused
+    // into that subtraction, what is left is the maximum's own rounding, past
+    // 2^31 more than exp2 holds)
+    return s * sc2;
   };
   // dims 8 r + 2 B, + 1 of the lane's four tokens; the scale byte is moved to
   // the exponent, the bits around it do not count
@@ -215,7 +219,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
     }
     float mc = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])),
                      fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    mc = fmaxf(m, over_column(mc, [](float a, float b) { return fmaxf(a, b); }) * sc2);
+    mc = fmaxf(m, over_column(mc, [](float a, float b) { return fmaxf(a, b); }));
     if (__any(mc > m)) {
       const float c = __builtin_amdgcn_exp2f(m - mc);
       l *= c;
@@ -226,8 +230,8 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(fmaf(s0[e], sc2, -m));
-      p[4 + e] = __builtin_amdgcn_exp2f(fmaf(s1[e], sc2, -m));
+      p[e] = __builtin_amdgcn_exp2f(s0[e] - m);
+      p[4 + e] = __builtin_amdgcn_exp2f(s1[e] - m);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) l += p[e];

@@ -3,6 +3,7 @@ numbers, contexts and lists cut into many partitions."""
 import numpy as np
 import pytest
 
+from oracle import gemv as og
 from paper_2609_13592_amd import binding as bd
 from tests.gpu_util import dev_f32, dev_u16, host_u16, stream, sync, to_dev_u16
 from tests.test_gpu_kv4 import attention
@@ -48,5 +49,39 @@ def test_nan_shows_in_any_number_of_partitions(gpu_ctx, fmt, H, Hq, blocks):
         for o, before in zip(rows(), clean):
             assert np.array_equal(np.isnan(o).all(2), want)
             assert np.array_equal(o[~want].view(np.uint32), before[~want].view(np.uint32))
+    finally:
+        c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("H,Hq", [(2, 8), (1, 8)])
+@pytest.mark.parametrize("blocks", [4, 70])
+@pytest.mark.parametrize("size", [1, 2 ** 15, 2 ** 20, 2 ** 55])
+def test_scores_of_any_size(gpu_ctx, fmt, H, Hq, blocks, size):
+    """Scores 253 * 32 * size * size * a, a of 0, 1, -6 .., exact in fp32 however they are
+    summed: far apart, so that the row is the value of the token with the
+    largest, or the mean of the two that have it."""
+    rng = np.random.default_rng(blocks)
+    c = Cache(gpu_ctx, rng, fmt, [16 * blocks, 16 * blocks - 3], H, Hq)
+    try:
+        c.q[:] = 0
+        d = rng.integers(0, 128, size=Hq)
+        c.q[:, np.arange(Hq), d] = og.f32_to_bf16(np.float32(32 * 253 * size))
+        best = np.zeros((2, H, 2), int)
+        for b in range(2):
+            k = rng.choice(np.array([0, 0.5, 1, -1, -6], np.float32), size=c.k[b].shape)
+            v = rng.choice(np.array([0, 0.5, 1, -1, -6], np.float32), size=c.k[b].shape)
+            best[b] = rng.integers(0, len(k), size=(H, 2))
+            for h in range(H):
+                k[best[b, h], h] = 6
+            c.k[b][:], c.v[b][:] = og.f32_to_bf16(k * np.float32(size)), og.f32_to_bf16(v)
+        c.write()
+        lists = np.tile(np.arange(blocks, dtype=np.int32), (2, H, 1))
+        for o in (c.attend(lists), attention(gpu_ctx, c.pool, 0, c.q, c.tables, c.lens)):
+            for b in range(2):
+                v = c.meaning(c.v[b])
+                for h in range(Hq):
+                    g = h // (Hq // H)
+                    assert np.array_equal(o[b, h], v[np.unique(best[b, g]), g].mean(0)), (b, h)
     finally:
         c.close()
