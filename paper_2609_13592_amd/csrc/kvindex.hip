@@ -101,6 +101,13 @@ __device__ __forceinline__ i16x2 over_rows2(i16x2 v, F f) {
   }));
 }
 
+// v in whole steps of 1 / scale, rounded up: one step at least for a positive v
+// (the product is 0 where it is below every fp32 number).
+__device__ __forceinline__ int steps_up(float v, float scale) {
+  const int n = static_cast<int>(ceilf(v * scale));
+  return v > 0.f ? max(n, 1) : n;
+}
+
 // The larger magnitude, as bf16 bits, of extremes hi (largest) and lo
 // (smallest) in both halves.
 __device__ __forceinline__ uint32_t magnitude(i16x2 hi, i16x2 lo) {
@@ -187,10 +194,10 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P) {
       const int e = bad ? kNotFinite : step_exponent(amax);
       const float scale = pow2f(bad ? 0 : -e);
       const uint32_t hx = values_of(mx[0]), hn = values_of(mn[0]);
-      const char2 hi = {static_cast<signed char>(ceilf(lo_bf16(hx) * scale)),
-                        static_cast<signed char>(ceilf(hi_bf16(hx) * scale))};
-      const char2 lo = {static_cast<signed char>(ceilf(lo_bf16(hn) * -scale)),
-                        static_cast<signed char>(ceilf(hi_bf16(hn) * -scale))};
+      const char2 hi = {static_cast<signed char>(steps_up(lo_bf16(hx), scale)),
+                        static_cast<signed char>(steps_up(hi_bf16(hx), scale))};
+      const char2 lo = {static_cast<signed char>(steps_up(-lo_bf16(hn), scale)),
+                        static_cast<signed char>(steps_up(-hi_bf16(hn), scale))};
       int8_t* const o = out + 32 * qd + 2 * r;
       *reinterpret_cast<char2*>(o) = bad ? char2{0, 0} : hi;
       *reinterpret_cast<char2*>(o + kD) = bad ? char2{0, 0} : lo;
@@ -235,9 +242,8 @@ __global__ __launch_bounds__(256) void index_update_kernel(IndexParams P) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t v = values_of(qd == 0 ? mx[j] : mn[j]);
-          const float sg = qd == 0 ? scale : -scale;
-          const int p = static_cast<int>(ceilf(lo_bf16(v) * sg));
-          const int q = static_cast<int>(ceilf(hi_bf16(v) * sg));
+          const int p = steps_up(qd == 0 ? lo_bf16(v) : -lo_bf16(v), scale);
+          const int q = steps_up(qd == 0 ? hi_bf16(v) : -hi_bf16(v), scale);
           w[j / 2] |= ((static_cast<uint32_t>(p) & 255u) | (static_cast<uint32_t>(q) & 255u) << 8)
                       << (16 * (j % 2));
         }

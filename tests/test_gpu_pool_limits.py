@@ -85,3 +85,26 @@ def test_scores_of_any_size(gpu_ctx, fmt, H, Hq, blocks, size):
                     assert np.array_equal(o[b, h], v[np.unique(best[b, g]), g].mean(0)), (b, h)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("small", [-149 + 54, -101, -120])
+def test_summaries_round_outwards_at_any_ratio(gpu_ctx, fmt, small):
+    """Keys 2^60 in some dims beside 2^small in the others, of either sign: a
+    step of 2^54 (a product of 2^(small - 54) is no fp32 number) still has the
+    small ones within [-1, 0] or [0, 1]."""
+    rng = np.random.default_rng(1)
+    c = Cache(gpu_ctx, rng, fmt, [100, 33, 1], 2, 8)
+    try:
+        for k in c.k:
+            x = rng.choice(np.array([1, -1, 0.5], np.float32), size=k.shape) * np.float32(2.0 ** small)
+            for t in range(0, len(k), 16):  # one sign a dim and block: both bounds at 0 and beyond
+                x[t:t + 16] = np.abs(x[t:t + 16]) * rng.choice(np.array([1, -1, 1], np.float32), size=x.shape[1:])
+            x[:, :, :32] = rng.choice(np.array([1, -1, 0.5], np.float32), size=x[:, :, :32].shape) * np.float32(2.0 ** 60)
+            k[:] = og.f32_to_bf16(x)
+        c.write()
+        bd.boost_kv_index_enable(c.pool)
+        c.index()
+        c.check_selection(2)
+    finally:
+        c.close()
