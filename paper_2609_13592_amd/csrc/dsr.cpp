@@ -97,7 +97,11 @@ int Dsr::alloc(uint64_t rid, uint32_t n, int32_t* out) {
     it = req_.emplace(rid, std::move(fresh)).first;
   }
   Req& r = it->second;
-  r.blocks.reserve(r.blocks.size() + n);
+  // room first (nothing changes without it), twice as much as before at least:
+  // reserve gives no more than it is asked for, and a decoding request comes
+  // back for every block
+  if (r.blocks.capacity() < r.blocks.size() + n)
+    r.blocks.reserve(std::max(r.blocks.size() + n, 2 * r.blocks.capacity()));
   for (uint32_t i = 0; i < n; ++i) {
     out[i] = take(r);
     r.blocks.push_back(out[i]);
