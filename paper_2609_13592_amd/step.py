@@ -57,16 +57,22 @@ class Dims:
 class DecodeModel:
     def __init__(self, ctx: int, dims: Dims, batch: int, max_blocks: int, pool: int,
                  matrices: dict, norms: dict, fold_slices: bool = True, top_blocks: int = 0,
-                 first_blocks: int = 1, last_blocks: int = 2):
+                 first_blocks: int | None = None, last_blocks: int | None = None):
         """matrices: name -> placed tensor handle for 'embed', 'lm_head' and
         '<kind>.<layer>'; norms: name -> device bf16 tensor for 'norm1.<l>',
         'norm2.<l>', 'norm_f'.  fold_slices: hand the split-K slices of qkv,
         o and down to their consumers (False: every projection reduces its
         own).  top_blocks: blocks that each KV head attends to, the context's
-        first_blocks and last_blocks always among them (0: the whole context).
+        first_blocks and last_blocks always among them (0: the whole context);
+        by default its last two and its first, as far as top_blocks goes.
         The summaries of earlier tokens (a prompt's) are the caller's to bring
         up to date, with boost_kv_index_update on every layer."""
         import torch
+        last = min(2, top_blocks) if last_blocks is None else last_blocks
+        first = max(0, min(1, top_blocks - last)) if first_blocks is None else first_blocks
+        # what select refuses, before anything is enabled or appended
+        if top_blocks and not (first >= 0 and last >= 0 and first + last <= top_blocks):
+            raise ValueError(f"the first {first} and the last {last} of {top_blocks} blocks")
         self.ctx, self.dims, self.B, self.mb, self.pool = ctx, dims, batch, max_blocks, pool
         self.mat, self.norms = matrices, norms
         D = dims
@@ -94,7 +100,7 @@ class DecodeModel:
         self.act = torch.zeros((B, D.ffn), dtype=b16, device=dev)
         self.logits = torch.zeros((B, D.vocab), dtype=f32, device=dev)
         self.ids = torch.zeros((B,), dtype=torch.int32, device=dev)
-        self.top, self.first, self.last = top_blocks, first_blocks, last_blocks
+        self.top, self.first, self.last = top_blocks, first, last
         if top_blocks:
             bd.boost_kv_index_enable(pool)
             self.scores = torch.zeros((B, D.hkv, max_blocks), dtype=f32, device=dev)

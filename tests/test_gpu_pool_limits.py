@@ -4,10 +4,12 @@ import numpy as np
 import pytest
 
 from oracle import gemv as og
+from oracle import select as osel
 from paper_2609_13592_amd import binding as bd
-from tests.gpu_util import dev_f32, dev_u16, host_u16, stream, sync, to_dev_u16
+from paper_2609_13592_amd.step import Dims
 from tests.test_gpu_kv4 import attention
-from tests.test_gpu_sparse import Cache, rand_u16
+from tests.test_gpu_sparse import Cache
+from tests.test_gpu_step_cache import Run
 
 pytestmark = pytest.mark.gpu
 FORMATS = [bd.KV_BF16, bd.KV_FP4]
@@ -108,3 +110,21 @@ def test_summaries_round_outwards_at_any_ratio(gpu_ctx, fmt, small):
         c.check_selection(2)
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("top", [1, 2, 3])
+def test_a_step_over_the_fewest_blocks(gpu_ctx, fmt, top):
+    """The blocks that are always taken by default, as far as the list goes:
+    the last two, then the first."""
+    dims = Dims(layers=2, d=512, hq=8, hkv=2, hd=128, ffn=384, vocab=500)
+    r = Run(gpu_ctx, dims, fmt, [1, 17, 300], top)
+    try:
+        ids, logits = r.step()
+        assert np.all(np.isfinite(logits)) and np.array_equal(ids, logits.argmax(1))
+        q, lists = r.model.q.cpu().double().numpy(), r.model.sel.cpu().numpy()
+        for b, (k, _) in enumerate(r.held(1)):  # the last layer's
+            want = osel.select(osel.scores(q[b], k), top, top > 2, min(top, 2))
+            assert np.array_equal(lists[b], want), b
+    finally:
+        r.close()
