@@ -649,9 +649,10 @@ int boost_kv_index_update(boost_ctx* ctx, const boost_kv_pool* p, int layer,
   const IndexParams P{pages, p->d_index + at * kSum, p->d_index + blocks * kSum + at, block_tables,
                       starts, ends, B, H, static_cast<int>(p->geom.nb), max_blocks};
   // blocks that max_tokens new tokens can touch, one wavefront each (a
-  // request with more has its wavefronts go round)
-  const int64_t touched = std::min<int64_t>((static_cast<int64_t>(max_tokens) + 2 * kT - 2) / kT,
-                                            max_blocks);
+  // request with more has its wavefronts go round; 2^22 of them are as many as
+  // any card has work for, and a grid counts its threads in 32 bits)
+  const int64_t touched = std::min<int64_t>({(static_cast<int64_t>(max_tokens) + 2 * kT - 2) / kT,
+                                             max_blocks, 1 << 22});
   const int chunks = static_cast<int>((touched + 3) / 4);
   if (H > 65535 || B > 65535) return fail(BOOST_EINVAL, "grid too large");
   const auto kernel = p->format == BOOST_KV_FP4 ? index_update_kernel<true>
@@ -683,7 +684,9 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   const SelectParams P{p->d_index + at * kSum, p->d_index + blocks * kSum + at,
                        static_cast<const uint16_t*>(q), block_tables, ctx_lens, scores, sel, B, H,
                        Hq, static_cast<int>(p->geom.nb), max_blocks, top_k, n_first, n_last};
-  const int chunks = (max_blocks + kScoreBlocks - 1) / kScoreBlocks;
+  // a context has at most kMaxTop blocks, however wide the table is (block
+  // numbers stay far below 2^31)
+  const int chunks = (std::min(max_blocks, kMaxTop) + kScoreBlocks - 1) / kScoreBlocks;
   if (H > 65535 || B > 65535 || static_cast<int64_t>(B) * H > 0x7fffffff)
     return fail(BOOST_EINVAL, "grid too large");
   const auto s = static_cast<hipStream_t>(stream);

@@ -7,6 +7,7 @@ from oracle import gemv as og
 from oracle import select as osel
 from paper_2609_13592_amd import binding as bd
 from paper_2609_13592_amd.step import Dims
+from tests.gpu_util import stream, sync, to_dev_u16
 from tests.test_gpu_kv4 import attention
 from tests.test_gpu_sparse import Cache
 from tests.test_gpu_step_cache import Run
@@ -128,3 +129,31 @@ def test_a_step_over_the_fewest_blocks(gpu_ctx, fmt, top):
             assert np.array_equal(lists[b], want), b
     finally:
         r.close()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("wide", [2 ** 26 + 5, 2 ** 31 - 1])
+def test_tables_as_wide_as_an_int32_goes(gpu_ctx, fmt, wide):
+    """A table and scores of up to 8 GiB each: the launches follow what a
+    context can have, and block numbers do not overflow at the table's end."""
+    import torch
+    rng = np.random.default_rng(3)
+    c = Cache(gpu_ctx, rng, fmt, [1000], 1, 4)
+    try:
+        c.write()
+        bd.boost_kv_index_enable(c.pool)
+        table = torch.full((wide,), -1, dtype=torch.int32, device="cuda")
+        table[:c.mb] = torch.from_numpy(c.tables[0]).cuda()
+        i32 = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+        bd.boost_kv_index_update(gpu_ctx, c.pool, 0, table, wide, i32(0), i32(1000), 1, 2 ** 31 - 1, stream())
+        scores = torch.full((wide,), 77.0, dtype=torch.float32, device="cuda")
+        sel = i32(*[99] * 9)
+        bd.boost_kv_select(gpu_ctx, c.pool, 0, to_dev_u16(c.q), 1, 4, table, wide, i32(1000), 9, 1, 2, scores,
+                           sel, stream())
+        sync()
+        want = osel.scores(og.bf16_to_f32(c.q[0]).astype(np.float64), c.meaning(c.k[0]))
+        assert np.array_equal(scores[:63].cpu().numpy()[None], want)
+        assert bool((scores[63:] == 77.0).all())
+        assert np.array_equal(sel.cpu().numpy()[None], osel.select(want, 9, 1, 2))
+    finally:
+        c.close()
