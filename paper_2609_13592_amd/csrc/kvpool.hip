@@ -581,7 +581,7 @@ int boost_kv_read(boost_ctx* ctx, const boost_kv_pool* p, int layer, const int32
 
 int boost_kv_copy_blocks(boost_ctx* ctx, const boost_kv_pool* p, int layer0, int n_layers,
                          const int32_t* src, const int32_t* dst, int n, void* stream) {
-  if (!ctx || !p || !src || !dst) return fail(BOOST_EINVAL, "null argument");
+  if (!ctx || !p || (n > 0 && (!src || !dst))) return fail(BOOST_EINVAL, "null argument");
   if (int rc = kv_device(p)) return rc;
   if (layer0 < 0 || n_layers < 1 ||
       static_cast<int64_t>(layer0) + n_layers > static_cast<int64_t>(p->cfg.layers))

@@ -157,3 +157,17 @@ def test_tables_as_wide_as_an_int32_goes(gpu_ctx, fmt, wide):
         assert np.array_equal(sel.cpu().numpy()[None], osel.select(want, 9, 1, 2))
     finally:
         c.close()
+
+
+def test_a_copy_of_nothing(gpu_ctx):
+    """n = 0 does nothing, with or without arrays; pairs need them."""
+    c = Cache(gpu_ctx, np.random.default_rng(0), bd.KV_BF16, [1], 1, 1)
+    try:
+        call = bd.load().boost_kv_copy_blocks
+        some = np.zeros(1, np.int32)
+        for src, dst in ((None, None), (some.ctypes.data, None), (some.ctypes.data, some.ctypes.data)):
+            assert call(gpu_ctx, c.pool, 0, 1, src, dst, 0, stream()) == bd.OK
+        assert call(gpu_ctx, c.pool, 0, 1, None, some.ctypes.data, 1, stream()) == bd.EINVAL
+        assert call(gpu_ctx, c.pool, 0, 1, some.ctypes.data, None, 1, stream()) == bd.EINVAL
+    finally:
+        c.close()
