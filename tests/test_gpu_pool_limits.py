@@ -8,7 +8,7 @@ from oracle import select as osel
 from paper_2609_13592_amd import binding as bd
 from paper_2609_13592_amd.step import Dims
 from tests.gpu_util import stream, sync, to_dev_u16
-from tests.test_gpu_kv4 import attention
+from tests.test_gpu_kv4 import attention, check, fill, make, new_pool
 from tests.test_gpu_sparse import Cache
 from tests.test_gpu_step_cache import Run
 
@@ -171,3 +171,37 @@ def test_a_copy_of_nothing(gpu_ctx):
         assert call(gpu_ctx, c.pool, 0, 1, some.ctypes.data, None, 1, stream()) == bd.EINVAL
     finally:
         c.close()
+
+
+@pytest.mark.parametrize("Hq,H,B,hi,mode,M", [(32, 8, 70, 3000, bd.KV_ALL_HBM, 0), (4, 1, 70, 3000, bd.KV_ALL_HBM, 0),
+                                              (16, 2, 130, 2700, bd.KV_LPP, 2), (8, 1, 300, 2600, bd.KV_LPP, 2),
+                                              (10, 5, 65, 4000, bd.KV_ALL_HOST, 0)])
+def test_4bit_partitions_of_many_requests(gpu_ctx, Hq, H, B, hi, mode, M):
+    """More than 64 requests in tables of more than 160 blocks: the one 4-bit
+    kernel that searches its items by barriers (to 160 blocks contexts stay
+    whole, up to 64 requests wavefronts search), over one and two rounds of 256
+    requests, up to four query heads and eight, pages on host and not."""
+    rng = np.random.default_rng(B + hi)
+    lens = rng.integers(1, hi, size=B, endpoint=True)
+    lens[0] = hi
+    lens[[2, B - 1]] = 0
+    lens[5:9] = [1, 16, 17, 2561]
+    mb, nb = (hi + 15) // 16, int(((lens + 15) // 16).sum())
+    assert mb > 160
+    tables, ks, vs, q = make(rng, lens, H, Hq, nb, mb)
+    pool = new_pool(gpu_ctx, H, Hq, nb, M, mode, max_batch=B, max_blocks=mb)
+    try:
+        if mode != bd.KV_ALL_HBM:
+            assert bd.boost_kv_pool_info(pool)["host_pages_per_tensor"] > 0
+        fill(gpu_ctx, pool, 0, lens, tables, ks, vs)
+        o = attention(gpu_ctx, pool, 0, q, tables, lens)
+        check(o, q, ks, vs, lens)
+        assert np.array_equal(attention(gpu_ctx, pool, 0, q, tables, lens, bd.DTYPE_BF16), og.f32_to_bf16(o))
+        on = attention(gpu_ctx, pool, 0, q, tables, lens, fn=bd.boost_paged_attn_decode_noalloc)
+        assert np.array_equal(on.view(np.uint32), o.view(np.uint32))
+        # requests one by one, whose items wavefronts search
+        for b in (0, 1, 5, 8, B - 2):
+            one = attention(gpu_ctx, pool, 0, q[b:b + 1], tables[b:b + 1], lens[b:b + 1])
+            check(one, q[b:b + 1], ks[b:b + 1], vs[b:b + 1], lens[b:b + 1])
+    finally:
+        bd.boost_kv_pool_destroy(pool)
