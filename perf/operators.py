@@ -31,7 +31,7 @@ def listed():
         # a chat of one user: the call with the fewest work items
         {"name": "4-bit attention, one short", "kind": "attn4", "q_heads": 32, "kv_heads": 8, "batch": 1,
          "ctx_lo": 301, "ctx_hi": 301, "empty": False, "modulus": 0},
-        # the 64-request configuration of the bf16 pool, some of the cache on host
+        # the 64-request configuration of the bf16 pool (1/130 of a 4-bit tensor's 40 pages is less than one: all in HBM)
         {"name": "4-bit attention, batch 64", "kind": "attn4", "q_heads": 32, "kv_heads": 8, "batch": 64,
          "ctx_lo": 512, "ctx_hi": 4096, "empty": False, "modulus": 130},
         # eight query heads per KV head, ragged contexts down to one token, an empty one among them
