@@ -600,7 +600,9 @@ int boost_kv_read(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
  * scale <= 0 selects 1/sqrt(D).  A block id outside [0, nb_pool) at a
  * position inside the context is skipped: its 16 tokens are left out of the
  * softmax (no read, no weight), as if they were not in the context; a row
- * whose every token is skipped, or ctx_lens[b] = 0, gives a zero row.
+ * whose every token is skipped, or ctx_lens[b] = 0, gives a zero row.  A NaN
+ * among q and the keys that count makes its row NaN, however the context is
+ * partitioned.
  * 1 <= B <= max_batch,
  * Hq == q_heads of the pool, max_blocks <= max_blocks_per_seq.
  * Errors: EINVAL, ENODEV, EHIP. */
@@ -653,9 +655,9 @@ int boost_kv_index_enable(boost_kv_pool *pool);
  * largest and the smallest key, in whole steps of 2^e rounded outwards to 8
  * bits, e the smallest in [-126, 122] with max|k| <= 127 * 2^e.  Blocks outside
  * the table or the pool are skipped; a block with an infinity or a NaN among
- * its keys scores +inf.  starts, ends: device int32 [B].  max_tokens is the
- * largest ends - starts (it sizes the launch; larger ranges are done all the
- * same).  Two requests must not update the same block in one call with other
+ * its keys scores +inf.  starts, ends: device int32 [B].  max_tokens (1 at
+ * least) is the largest ends - starts (it sizes the launch; larger ranges are
+ * done all the same).  Two requests must not update the same block in one call with other
  * ends.  B up to 65535, here and in boost_kv_select.
  * Errors: EINVAL (also: no summaries), ENODEV, EHIP. */
 int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,

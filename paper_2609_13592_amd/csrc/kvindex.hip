@@ -692,8 +692,9 @@ int boost_kv_select(boost_ctx* ctx, const boost_kv_pool* p, int layer, const voi
   const auto s = static_cast<hipStream_t>(stream);
   // Tables of up to 512 blocks in one launch (whole steps: one request of 250
   // blocks 17.9 us, 19.5 with two launches; 64 of 250 43.6 and 45.6; 24 of 500
-  // in 4 bits 20.5 and 22.1, four of them 18.9 and 18.2).  1000 blocks to a
-  // workgroup: one request 25.9 and 20.4.
+  // in 4 bits 20.5 and 22.1).  Few lists of the widest of these tables lose a
+  // little (four of 500 18.9 and 18.2), which is accepted for a rule on the
+  // width alone.  1000 blocks to a workgroup: one request 25.9 and 20.4.
   if (max_blocks <= 512) {
     if (max_blocks <= 256)
       hipLaunchKernelGGL(scores_select_kernel<4>, dim3(H, B), dim3(256), 0, s, P);
