@@ -282,8 +282,8 @@ int destroy(boost_kv_pool* p) {
 
 namespace bst {
 int kv_parts_for(const boost_kv_pool* p, int max_blocks) {
-  const int tokens = max_blocks * static_cast<int>(p->cfg.block_tokens);
-  return std::max(1, (tokens + kPartTokensMin - 1) / kPartTokensMin);
+  const int64_t tokens = static_cast<int64_t>(max_blocks) * p->cfg.block_tokens;
+  return static_cast<int>(std::max<int64_t>(1, (tokens + kPartTokensMin - 1) / kPartTokensMin));
 }
 
 int kv_device(const boost_kv_pool* p) {

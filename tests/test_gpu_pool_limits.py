@@ -205,3 +205,23 @@ def test_4bit_partitions_of_many_requests(gpu_ctx, Hq, H, B, hi, mode, M):
             check(one, q[b:b + 1], ks[b:b + 1], vs[b:b + 1], lens[b:b + 1])
     finally:
         bd.boost_kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_pool_for_the_longest_contexts(gpu_ctx, fmt):
+    """max_blocks_per_seq 2^27, what int32 tokens fill (16 GiB of scratch for one
+    query head): calls over short tables run."""
+    rng = np.random.default_rng(2)
+    lens = np.array([1000])
+    tables, ks, vs, q = make(rng, lens, 1, 1, 63, 63)
+    pool = new_pool(gpu_ctx, 1, 1, 63, max_batch=1, max_blocks=2 ** 27, fmt=fmt)
+    small = new_pool(gpu_ctx, 1, 1, 63, max_batch=1, max_blocks=63, fmt=fmt)
+    try:
+        rows = []
+        for p in (pool, small):
+            fill(gpu_ctx, p, 0, lens, tables, ks, vs)
+            rows.append(attention(gpu_ctx, p, 0, q, tables, lens))
+        assert np.any(rows[0]) and np.array_equal(rows[0].view(np.uint32), rows[1].view(np.uint32))
+    finally:
+        bd.boost_kv_pool_destroy(pool)
+        bd.boost_kv_pool_destroy(small)
