@@ -87,17 +87,25 @@ __device__ __forceinline__ float row16_sum(float v) {
   return v;
 }
 
+// Maxima and scores stay as the dot products are, and a weight is
+// exp2((score - max) * sc2), sc2 = scale * log2(e): the difference is taken
+// first, so the largest score has weight 1 at any size, and no rounding of a
+// large scaled score is left in it.
+__device__ __forceinline__ float weight(float score, float max, float sc2) {
+  return __builtin_amdgcn_exp2f((score - max) * sc2);
+}
+
 // merge running state (m, l, acc) with another one; symmetric in its operands
 template <int G>
 __device__ __forceinline__ void merge_state(float* m, float* l, float (*acc)[8],
                                             const float* m2, const float* l2,
-                                            const float (*acc2)[8]) {
+                                            const float (*acc2)[8], float sc2) {
 #pragma unroll
   for (int j = 0; j < G; ++j) {
     const float M = fmaxf(m[j], m2[j]);
     if (M == -INFINITY) continue;  // both empty
-    const float c1 = __builtin_amdgcn_exp2f(m[j] - M);  // m = -inf gives 0
-    const float c2 = __builtin_amdgcn_exp2f(m2[j] - M);
+    const float c1 = weight(m[j], M, sc2);  // m = -inf gives 0
+    const float c2 = weight(m2[j], M, sc2);
     l[j] = l[j] * c1 + l2[j] * c2;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[j][e] = acc[j][e] * c1 + acc2[j][e] * c2;
@@ -124,7 +132,7 @@ __device__ __forceinline__ void pair_of(float v, float& lo, float& hi) {
 // The running states of the lane pairs D apart merged, lower lane's state
 // first; afterwards both lanes hold the result.
 template <int G, int D>
-__device__ __forceinline__ void slot_merge(float* m, float* l, float (*acc)[8]) {
+__device__ __forceinline__ void slot_merge(float* m, float* l, float (*acc)[8], float sc2) {
   float m2[G], l2[G], a2[G][8];
 #pragma unroll
   for (int j = 0; j < G; ++j) {
@@ -133,7 +141,7 @@ __device__ __forceinline__ void slot_merge(float* m, float* l, float (*acc)[8]) 
 #pragma unroll
     for (int e = 0; e < 8; ++e) pair_of<D>(acc[j][e], acc[j][e], a2[j][e]);
   }
-  merge_state<G>(m, l, acc, m2, l2, a2);
+  merge_state<G>(m, l, acc, m2, l2, a2, sc2);
 }
 
 // V of a token that does not count: zeros, whatever its slot holds.
@@ -141,16 +149,7 @@ __device__ __forceinline__ uint4 live(const uint4& v, bool valid) {
   return make_uint4(valid ? v.x : 0, valid ? v.y : 0, valid ? v.z : 0, valid ? v.w : 0);
 }
 
-// A score in the log2 domain, rounded by itself: the largest minus itself is then
-// 0 at any size.  (Fused into the subtraction of the maximum, what is left is the
-// maximum's own rounding, past 2^31 more than exp2 holds.)
-__device__ __forceinline__ float scaled(float dot, float sc2) {
-#pragma clang fp contract(off)
-  return dot * sc2;
-}
-
-// Online-softmax update of one token slot with U blocks.  Scores are in the
-// log2 domain (q . k * scale * log2 e), so exp2 is one instruction.  With
+// Online-softmax update of one token slot with U blocks.  With
 // MASKED false every token is valid; otherwise invalid tokens have score -inf
 // and contribute nothing.
 template <int G, int U, bool MASKED, typename AfterK>
@@ -166,7 +165,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
       d = dot2(qp[j][1], kb[u].y, d);
       d = dot2(qp[j][2], kb[u].z, d);
       d = dot2(qp[j][3], kb[u].w, d);
-      d = scaled(row16_sum(d), sc2);  // q . k over the 16 lanes of the token row
+      d = row16_sum(d);  // q . k over the 16 lanes of the token row
       sc[u][j] = (!MASKED || valid[u]) ? d : -INFINITY;
     }
   after_k();  // the K registers are free from here on
@@ -176,7 +175,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
 #pragma unroll
     for (int u = 0; u < U; ++u) mc = fmaxf(mc, sc[u][j]);
     if (MASKED && mc == -INFINITY) continue;  // nothing valid yet
-    const float c = __builtin_amdgcn_exp2f(m[j] - mc);  // exp2(-inf) = 0 at start
+    const float c = weight(m[j], mc, sc2);  // exp2(-inf) = 0 at start
     l[j] *= c;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[j][e] *= c;
@@ -192,7 +191,7 @@ __device__ __forceinline__ void consume(const uint32_t (*qp)[4], const uint4* kb
       // running max is still -inf
       const float p = (MASKED && sc[u][j] == -INFINITY)
                           ? 0.f
-                          : __builtin_amdgcn_exp2f(sc[u][j] - m[j]);
+                          : weight(sc[u][j], m[j], sc2);
       l[j] += p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[j][e] = fmaf(p, vf[e], acc[j][e]);
@@ -278,7 +277,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
         x = dot2(q[j].z, kb[u].z, x);
         d[j] = dot2(q[j].w, kb[u].w, x);
       }
-      const float f = scaled(score_of_lane_head<Q>(d, b0, b1), sc2);
+      const float f = score_of_lane_head<Q>(d, b0, b1);
       s[u][i] = (!MASKED || valid[u]) ? f : -INFINITY;
     }
     if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);  // (registers)
@@ -291,7 +290,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
 #pragma unroll
     for (int u = 0; u < U; ++u) mc = fmaxf(mc, s[u][i]);
     // nothing valid yet for this head: keep the state (factor 1)
-    c[i] = (MASKED && mc == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f(mh[i] - mc);
+    c[i] = (MASKED && mc == -INFINITY) ? 1.f : weight(mh[i], mc, sc2);
     lh[i] *= c[i];
     mh[i] = mc;
   }
@@ -305,7 +304,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
     float p[N], pj[G], vf[8];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      p[i] = (MASKED && s[u][i] == -INFINITY) ? 0.f : __builtin_amdgcn_exp2f(s[u][i] - mh[i]);
+      p[i] = (MASKED && s[u][i] == -INFINITY) ? 0.f : weight(s[u][i], mh[i], sc2);
       lh[i] += p[i];
     }
     bcast_groups<G>(p, pj);
@@ -320,7 +319,7 @@ __device__ __forceinline__ void consume_hd(Query query, const uint4* kb,
 
 // slot_merge for the head-distributed state: the factors once per head.
 template <int G, int D>
-__device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)[8]) {
+__device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)[8], float sc2) {
   constexpr int N = G / hd_group<G>();
   float c1[N], c2[N], c1j[G], c2j[G];
 #pragma unroll
@@ -330,8 +329,8 @@ __device__ __forceinline__ void slot_merge_hd(float* mh, float* lh, float (*acc)
     pair_of<D>(lh[i], l1, l2);
     const float M = fmaxf(m1, m2);
     // both empty: factors 1 on zero sums
-    c1[i] = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m1 - M);
-    c2[i] = M == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - M);
+    c1[i] = M == -INFINITY ? 1.f : weight(m1, M, sc2);
+    c2[i] = M == -INFINITY ? 1.f : weight(m2, M, sc2);
     lh[i] = l1 * c1[i] + l2 * c2[i];
     mh[i] = M;
   }
@@ -567,13 +566,13 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   // 16-apart pair, permlane32_swap the same for lanes 32 apart, so both
   // lanes of a pair merge the same two states in the same order
   if constexpr (kHD) {
-    slot_merge_hd<G, 16>(mh, lh, acc);
-    slot_merge_hd<G, 32>(mh, lh, acc);
+    slot_merge_hd<G, 16>(mh, lh, acc, sc2);
+    slot_merge_hd<G, 32>(mh, lh, acc, sc2);
     bcast_groups<G>(mh, m);  // every head's maximum and sum in every lane again
     bcast_groups<G>(lh, l);
   } else {
-    slot_merge<G, 16>(m, l, acc);
-    slot_merge<G, 32>(m, l, acc);
+    slot_merge<G, 16>(m, l, acc, sc2);
+    slot_merge<G, 32>(m, l, acc, sc2);
   }
   const int wave = tid >> 6, lane = tid & 63;
   if (lane < kLanesTok) {
@@ -605,7 +604,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
       float a2[1][8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) a2[0][e] = s_acc[w][j][dc * 8 + e];
-      merge_state<1>(&mj, &lj, aj, &m2, &l2, a2);
+      merge_state<1>(&mj, &lj, aj, &m2, &l2, a2, sc2);
     }
     if constexpr (ONE) {
       const float inv = lj != 0.f ? 1.f / lj : 0.f;  // nothing counted: zeros
@@ -637,8 +636,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
   }
 }
 
-// One wavefront per (request, query head): o = sum_p acc_p e^(m_p - M) /
-// sum_p l_p e^(m_p - M) over the request's partitions, in partition order.
+// One wavefront per (request, query head): o = sum_p acc_p w_p / sum_p l_p w_p
+// with w_p the weight of the partition's maximum, over the request's partitions, in partition order.
 __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   const int bh = blockIdx.x;  // b * Hq + h
   const int b = bh / P.Hq;
@@ -647,6 +646,7 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   const int n_blk = L <= 0 ? 0 : min(blocks_in(L), P.item_blocks);
   const int np = (n_blk + P.part_blocks - 1) / P.part_blocks;
   const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
+  const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
   // the largest partition maximum: one partition per lane, then across the
   // wavefront (a maximum is exact in any order)
   float M = -INFINITY;
@@ -680,7 +680,7 @@ __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
       // past np, or an empty partition (one of NaN scores alone has that
       // maximum too, and a NaN sum)
       if (mp[u] == -INFINITY && lp[u] == 0.f) continue;
-      const float w = __builtin_amdgcn_exp2f(mp[u] - M);  // maxima are in the log2 domain
+      const float w = weight(mp[u], M, sc2);
       den = fmaf(lp[u], w, den);
       o0 = fmaf(a[u].x, w, o0);
       o1 = fmaf(a[u].y, w, o1);
@@ -715,6 +715,7 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
   if (np == 1 && P.one_done) return;  // uniform: the row is written
   const int per = (np + W - 1) / W, beg = min(np, wave * per), end = min(np, beg + per);
   const int64_t base = static_cast<int64_t>(bh) * P.max_parts;
+  const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
   constexpr int kBatch = 8;
   float m = -INFINITY, den = 0.f, o0 = 0.f, o1 = 0.f;
   for (int p0 = beg; p0 < end; p0 += 64) {  // a lane's partition of this round
@@ -737,12 +738,12 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
     // as an empty one's), its sum is NaN
     const bool nan = ml.y != ml.y;
     if (M == -INFINITY && !__any(nan)) continue;  // uniform: nothing but empty partitions
-    const float c = __builtin_amdgcn_exp2f(m - M);  // m = -inf: 0
+    const float c = weight(m, M, sc2);  // m = -inf: 0
     den *= c;
     o0 *= c;
     o1 *= c;
     m = M;
-    const float w = nan ? ml.y : ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - M);
+    const float w = nan ? ml.y : ml.x == -INFINITY ? 0.f : weight(ml.x, M, sc2);
     const float wl = w * ml.y;
     for (int u0 = 0; u0 < n; u0 += kBatch) {
       if (u0 > 0) load(u0);
@@ -772,8 +773,7 @@ __global__ __launch_bounds__(64 * W) void attn_merge_wide(AttnParams P) {
   den = o0 = o1 = 0.f;
 #pragma unroll
   for (int w = 0; w < W; ++w) {
-    const float c = s_m[w] == -INFINITY && s_den[w] == 0.f ? 0.f
-                                                           : __builtin_amdgcn_exp2f(s_m[w] - M);
+    const float c = s_m[w] == -INFINITY && s_den[w] == 0.f ? 0.f : weight(s_m[w], M, sc2);
     den = fmaf(s_den[w], c, den);
     o0 = fmaf(s_o[w][lane].x, c, o0);
     o1 = fmaf(s_o[w][lane].y, c, o1);

@@ -159,7 +159,6 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
   };
   const float sc2 = P.scale * 1.4426950408889634f;  // log2(e)
   auto scores = [&](const Block4& x) {
-#pragma clang fp contract(off)
     const float ks = bst::fp4_scale(x.ks);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -168,10 +167,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
                        fp4_unpack<2>(x.k[i], ks), fp4_unpack<3>(x.k[i], ks)};
       s = mfma(a, bq[i], s);
     }
-    // rounded by itself, so that the largest minus itself is 0 at any size (fused
-    // into that subtraction, what is left is the maximum's own rounding, past
-    // 2^31 more than exp2 holds)
-    return s * sc2;
+    return s;
   };
   // dims 8 r + 2 B, + 1 of the lane's four tokens; the scale byte is moved to
   // the exponent, the bits around it do not count
@@ -221,7 +217,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
                      fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
     mc = fmaxf(m, over_column(mc, [](float a, float b) { return fmaxf(a, b); }));
     if (__any(mc > m)) {
-      const float c = __builtin_amdgcn_exp2f(m - mc);
+      const float c = __builtin_amdgcn_exp2f((m - mc) * sc2);
       l *= c;
 #pragma unroll
       for (int t = 0; t < 4; ++t) acc[t] *= c;
@@ -230,8 +226,9 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
     float p[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(s0[e] - m);
-      p[4 + e] = __builtin_amdgcn_exp2f(s1[e] - m);
+      // (the difference first: the largest score has weight 1 at any size)
+      p[e] = __builtin_amdgcn_exp2f((s0[e] - m) * sc2);
+      p[4 + e] = __builtin_amdgcn_exp2f((s1[e] - m) * sc2);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) l += p[e];
@@ -304,7 +301,7 @@ __global__ __launch_bounds__(64 * W) void attn4_partition(AttnParams P) {
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const float c = __builtin_amdgcn_exp2f(s_ml[w][j][0] - M);
+      const float c = __builtin_amdgcn_exp2f((s_ml[w][j][0] - M) * sc2);
       sum += s_ml[w][j][1] * c;
       f32x4 a = *reinterpret_cast<const f32x4*>(&s_acc[w][j][d4]);
       if constexpr (!EIGHT) a += *reinterpret_cast<const f32x4*>(&s_acc[w][j + 4][d4]);

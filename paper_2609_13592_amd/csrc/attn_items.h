@@ -70,7 +70,7 @@ struct AttnParams {
   int max_parts;             // stride of the partial buffers
   float scale;
   float* part_acc;  // [B * Hq * max_parts][D] unnormalised sums of p * v
-  float* part_ml;   // [B * Hq * max_parts][2] running max, sum of p
+  float* part_ml;   // [B * Hq * max_parts][2] running max of q . k, sum of p
   void* out;
   int out_bf16;
   int one_done;  // contexts of one partition are finished without the merge
