@@ -207,6 +207,27 @@ def test_4bit_partitions_of_many_requests(gpu_ctx, Hq, H, B, hi, mode, M):
         bd.boost_kv_pool_destroy(pool)
 
 
+@pytest.mark.parametrize("Hq,H,B,hi", [(64, 8, 40, 300), (40, 8, 33, 2560), (7, 1, 300, 90)])
+def test_4bit_whole_contexts_of_many_heads(gpu_ctx, Hq, H, B, hi):
+    """More than four query heads to a KV head, more (request, KV head) pairs
+    than compute units, tables of up to 160 blocks: one workgroup of four
+    wavefronts a pair, nothing to merge."""
+    rng = np.random.default_rng(B)
+    lens = rng.integers(1, hi, size=B, endpoint=True)
+    lens[:4] = [hi, 1, 0, 17]
+    lens[B - 1] = 0
+    mb, nb = (hi + 15) // 16, int(((lens + 15) // 16).sum())
+    tables, ks, vs, q = make(rng, lens, H, Hq, nb, mb)
+    pool = new_pool(gpu_ctx, H, Hq, nb, max_batch=B, max_blocks=mb)
+    try:
+        fill(gpu_ctx, pool, 0, lens, tables, ks, vs)
+        o = attention(gpu_ctx, pool, 0, q, tables, lens)
+        check(o, q, ks, vs, lens)
+        assert np.array_equal(attention(gpu_ctx, pool, 0, q, tables, lens, bd.DTYPE_BF16), og.f32_to_bf16(o))
+    finally:
+        bd.boost_kv_pool_destroy(pool)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_a_pool_for_the_longest_contexts(gpu_ctx, fmt):
     """max_blocks_per_seq 2^27, what int32 tokens fill (16 GiB of scratch for one
