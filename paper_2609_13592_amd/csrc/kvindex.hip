@@ -291,7 +291,7 @@ __device__ __forceinline__ int scores_from(const SelectParams& P, int b, int g, 
   // the lower and the upper 64 dims, then the negative ones)
   __shared__ uint32_t s_q[4][64][4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, qd = lane >> 4;
-  const int quarter = wave & 3;  // of the rounding of q (of eight wavefronts two do each)
+  const int quarter = wave & 3;  // of the rounding of q (of eight wavefronts two write the same of it)
   const int L = P.lens[b];  // (the ids do not wait for it)
   const int first = base + wave * kTiles * kTileBlocks;
   const int G = P.Hq / P.H;
