@@ -558,7 +558,8 @@ int boost_kv_request_blocks(const boost_kv_pool *pool, uint64_t request_id, int3
  * the blocks' summaries where the pool has them.  src, dst: HOST arrays, read
  * before the call returns.  A source may serve several destinations; a
  * destination comes once and is no source.  n = 0 does nothing.  Asynchronous
- * on `stream`; may be captured (a graph keeps the pairs of its capture).
+ * on `stream`; may be captured (a graph keeps the pairs of its capture, and
+ * copies summaries if the pool had them then).
  * Errors: EINVAL (layers, a block outside the pool, a destination twice or
  * among the sources), ENODEV, ENOMEM, EHIP. */
 int boost_kv_copy_blocks(boost_ctx *ctx, const boost_kv_pool *pool, int layer0, int n_layers,
@@ -657,8 +658,8 @@ int boost_kv_index_enable(boost_kv_pool *pool);
  * the table or the pool are skipped; a block with an infinity or a NaN among
  * its keys scores +inf.  starts, ends: device int32 [B].  max_tokens (1 at
  * least) is the largest ends - starts (it sizes the launch; larger ranges are
- * done all the same).  Two requests must not update the same block in one call with other
- * ends.  B up to 65535, here and in boost_kv_select.
+ * done all the same).  Two requests must not update the same block in one call
+ * with other ends.  B up to 65535, here and in boost_kv_select.
  * Errors: EINVAL (also: no summaries), ENODEV, EHIP. */
 int boost_kv_index_update(boost_ctx *ctx, const boost_kv_pool *pool, int layer,
                           const int32_t *block_tables, int max_blocks,

@@ -637,7 +637,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
 }
 
 // One wavefront per (request, query head): o = sum_p acc_p w_p / sum_p l_p w_p
-// with w_p the weight of the partition's maximum, over the request's partitions, in partition order.
+// with w_p the weight of the partition's maximum, over the request's
+// partitions, in partition order.
 __global__ __launch_bounds__(64) void attn_merge(AttnParams P) {
   const int bh = blockIdx.x;  // b * Hq + h
   const int b = bh / P.Hq;
